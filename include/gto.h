@@ -41,10 +41,12 @@ typedef enum {
   GTO_ERR_WORKSPACE = 3,   /* workspace allocation failed                                */
   GTO_ERR_CUDA = 4,        /* a CUDA runtime call failed                                 */
   GTO_ERR_NONFINITE = 5,   /* device status: a row's log-sum-exp was not finite          */
-  /* 6 is not used: no kernel of the library waits on anything                            */
+  GTO_ERR_TIMEOUT = 6,     /* device status: a wait inside gto_tree_attention ran out; the
+                              outputs of that call are unspecified                       */
   GTO_ERR_TOO_LARGE = 7,   /* gto_build_tree_noalloc: batch exceeds the fixed scratch    */
   GTO_ERR_BAD_INDEX = 8    /* device status: an index in a caller's table (d2t, a tree's
-                              rows, tokens or parents, a path's rows) was out of range; the
+                              rows, tokens or parents, a path's rows, a page table, the
+                              lengths of a batch) was out of range; the
                               entry was skipped, results that depend on it are unspecified  */
 } gto_status;
 
@@ -282,6 +284,161 @@ gto_status gto_kernel_timing(gto_ctx* ctx, int enable);
  * record: total_ms[i] = summed device time of kernel i, launches[i] = how many.  Both
  * arrays are HOST arrays of GTO_K_COUNT entries. */
 gto_status gto_kernel_times(gto_ctx* ctx, void* stream, double* total_ms, int64_t* launches);
+
+/* ------------------------------------------------------------------------------------------
+ * One decoding step over a draft tree (Sec. 2 of the paper: the target verifies the tree that
+ * policy G built, in one forward pass under the tree's mask).
+ *
+ *   gto_kv_append       puts the keys and values of a chunk of new tokens into a paged cache,
+ *                       with the rotation of their positions
+ *   gto_tree_attention  attention of the chunk over the cache and over itself
+ *   gto_verify_tree     which drafted tokens the target accepts, and the token after them
+ *   gto_kv_commit       moves the accepted tokens' cache entries together
+ *
+ * A batch has S sequences.  Sequence s brings a chunk of n = q_start[s+1] - q_start[s] tokens;
+ * kv_len[s] = L counts its cache entries, the chunk's among them, so the chunk owns entries
+ * base .. L-1 with base = L - n.  Without a tree the chunk's tokens follow one another (one
+ * token: plain decoding; many: a piece of a prompt).  With a tree the last n_nodes[s] tokens of
+ * the chunk are the nodes of a draft tree in the order of gto_tree's node lists, and the
+ * lead = n - n_nodes[s] tokens before them follow one another; the first level of the tree hangs
+ * below the last of them (or, with lead = 0, below entry base - 1).
+ * Entry t of sequence s lies in place t % page_size of page page_table[s][t / page_size].
+ *
+ * The functions take a gto_decode_ctx, which owns the workspace and a status word.  Calls
+ * through one context share them: order them (one stream, events), and give every stream or
+ * captured graph that may run at the same time a context of its own.  The calls can be
+ * captured into a CUDA graph; lengths, tables and trees are read on the device at replay.
+ * Every index is checked on the device before it is followed: a sequence with an inconsistent
+ * q_start, kv_len, n_nodes or page_table entry is reported (GTO_ERR_BAD_INDEX) and skipped. */
+
+typedef struct gto_decode_ctx gto_decode_ctx;
+
+enum {
+  GTO_DECODE_ROPE_INTERLEAVED = 1u, /* rotate the pairs (2i, 2i+1) instead of (i, i + rope_dims/2) */
+  GTO_DECODE_CONTEXT_ROWS = 2u /* gto_verify_tree reads target rows in the layout of
+                                  gto_tree_reward, [S, R, V_target] with R = 1 + (D-1)k, through
+                                  node_depth and node_slot; default: [S, 1+g, V_target], row 0
+                                  after the root, row 1 + n after node n                        */
+};
+
+typedef struct {
+  int32_t S;          /* most sequences of a call                                         */
+  int32_t T;          /* most tokens of a call                                            */
+  int32_t g;          /* nodes of a draft tree (row length of the node arrays); 0: none   */
+  int32_t D;          /* most levels of a tree                                            */
+  int32_t k;          /* frontier slots per level, with GTO_DECODE_CONTEXT_ROWS only       */
+  int32_t n_q_heads, n_kv_heads, head_dim;  /* n_kv_heads = 0: no cache (verification only) */
+  int32_t page_size, n_pages, max_pages;    /* entries of a page, pages, row of page_table  */
+  int32_t kv_dtype;   /* gto_dtype of queries, keys, values, cache and output             */
+  int32_t rope_dims;  /* leading dimensions of a head that are rotated; 0: none            */
+  int32_t V_draft, V_target, logit_dtype;   /* V_target = 0: no verification               */
+  float softmax_scale;
+  float norm_eps;     /* epsilon of the optional query / key norms                         */
+  uint32_t flags;
+} gto_decode_config;
+
+/* Device pointers of a batch. */
+typedef struct {
+  int32_t S, T;               /* sequences; tokens the token arrays have room for           */
+  const int32_t* q_start;     /* [S+1] first token of every chunk; tokens from q_start[S] on
+                                 belong to no sequence and are left alone                   */
+  const int32_t* kv_len;      /* [S]                                                        */
+  const int32_t* page_table;  /* [S, max_pages]                                             */
+  const int32_t* n_nodes;     /* [S] tree nodes of each chunk, 0..g; NULL: g everywhere     */
+  const uint64_t* node_mask;  /* [S, g, ceil(g/64)] as in gto_tree; NULL: no trees          */
+  const int32_t* node_depth;  /* [S, g] as in gto_tree, for gto_kv_append; NULL: no trees   */
+} gto_batch;
+
+/* Paged keys and values.  Element (layer, page, entry, head, :) starts at the sum of the
+ * indices times the strides; the head_dim values of a head are contiguous.  Strides count
+ * elements, multiples of 16 bytes. */
+typedef struct {
+  void* k;
+  void* v;
+  int64_t k_page, k_entry, k_head, k_layer;
+  int64_t v_page, v_entry, v_head, v_layer;
+  int32_t n_layers;  /* gto_kv_commit works on all of them; the other calls on layer 0      */
+} gto_kv_cache;
+
+/* Trees to verify: arrays of gto_tree, restricted to the S trees (row length g). */
+typedef struct {
+  int32_t S;
+  const int32_t* node_token;   /* [S, g] */
+  const int32_t* node_parent;  /* [S, g] */
+  const int32_t* node_depth;   /* [S, g] with GTO_DECODE_CONTEXT_ROWS, else NULL */
+  const int32_t* node_slot;    /* [S, g] with GTO_DECODE_CONTEXT_ROWS, else NULL */
+  const int32_t* n_nodes;      /* [S] nodes of each tree, 0..g; NULL: g */
+} gto_draft_tree;
+
+typedef struct {
+  int32_t* accept_len;  /* [S] accepted drafted tokens                                      */
+  int32_t* path_node;   /* [S, D] their list positions; -1 beyond accept_len                */
+  int32_t* token;       /* [S, D+1] their target-vocabulary ids, then the token that follows
+                           them (-1 if the last node has no target row); -1 beyond          */
+} gto_verdict;
+
+/* Limits: 0 <= g <= 128; 1 <= D <= 16; n_q_heads a multiple of n_kv_heads, at most 128 of
+ * them per key head; head_dim a multiple of 16, at most 256; rope_dims a multiple of 16, at
+ * most head_dim; max_pages * page_size < 2^31; V * sizeof(logit) a multiple of 16 for the target
+ * vocabulary and at most 1.5 MB; g <= V_draft <= V_target. */
+gto_status gto_decode_create(gto_decode_ctx** ctx, const gto_decode_config* cfg, int device);
+gto_status gto_decode_destroy(gto_decode_ctx* ctx);
+
+/* Keys and values of the batch into the cache, queries rotated on the way.  q, k, v: rows of
+ * n_heads * head_dim contiguous elements, row t at t * stride (elements, a multiple of 16
+ * bytes: they may be slices of one projection); q_out: dense [T, n_q_heads, head_dim], may be
+ * q itself where q is dense; q and q_out may both be NULL.  Token i of the lead has position
+ * base + i, node a of the tree base + lead - 1 + node_depth[a].
+ * q_norm / k_norm ([head_dim], kv_dtype, or NULL): the head is first scaled to unit mean
+ * square and multiplied by the weights.  Then the pair (x_i, x_{i + rope_dims/2}) is rotated by
+ * the angle position * inv_freq[i] (inv_freq: [rope_dims/2] fp64; the angle is formed in fp64,
+ * so that far positions keep their phase).  Everything in fp32, rounded once.  Values are
+ * copied.  Two sequences must not own the same cache entry. */
+gto_status gto_kv_append(gto_decode_ctx* ctx, const gto_batch* batch, const gto_kv_cache* cache,
+                         const void* q, int64_t q_stride, const void* k, int64_t k_stride,
+                         const void* v, int64_t v_stride, void* q_out, const double* inv_freq,
+                         const void* q_norm, const void* k_norm, void* stream);
+
+/* out[t] = sum over visible entries e of softmax_e(softmax_scale q_t . k_e) v_e, for every token
+ * of the batch and every query head (query head h reads key head h / (n_q_heads / n_kv_heads)).
+ * A token of the lead sees the entries up to its own; node a of a tree sees every entry before
+ * the tree and the nodes in row a of node_mask.  A row that sees nothing gives zeros.  q as in
+ * gto_kv_append; out: dense [T, n_q_heads, head_dim]; lse ([T, n_q_heads] fp32 or NULL) receives
+ * the log-sum-exp of the row's scaled scores, -inf for a row that sees nothing.  Rows of tokens
+ * that belong to no sequence are left as they were.  out must not overlap q. */
+gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const gto_kv_cache* cache,
+                              const void* q, int64_t q_stride, void* out, float* lse, void* stream);
+
+/* Verification of drafted tokens against the target's probabilities.  The walk starts at the root.
+ * At a context with target logits z let p = softmax(z / temperature[s]) and M = 1; the drafted
+ * children x_1, x_2, ... of the context are tried in list order: child x is accepted if
+ * u_node[x] * M < p(x), else p(x) is taken out: M -= p(x), p(x) = 0 (a child with the token of an
+ * earlier one therefore cannot be accepted).  An accepted child becomes the context.  When none
+ * is accepted the step's last token is drawn from what is left: the smallest id v with
+ * sum_{w <= v} p(w) > u_bonus[s] * M.  The drafted tokens are point proposals (policy G takes
+ * the k best, it does not sample), so the accepted tokens and the last one together follow the
+ * target's distribution exactly.  temperature 0: a child is accepted if its token is the
+ * arg-max (lowest id on ties), and the last token is the arg-max.
+ * target: [S, 1+g, V_target] (see GTO_DECODE_CONTEXT_ROWS); d2t: [V_draft] or NULL (identity,
+ * needs V_draft == V_target); temperature, u_bonus: [S] fp32; u_node: [S, g] fp32; the uniforms
+ * are given by the caller, in [0, 1) (clamped to it).  Sums are fp64.  A sequence whose visited
+ * rows hold NaN or +inf, or nothing but -inf, or whose temperature is negative or not finite,
+ * is reported (GTO_ERR_NONFINITE); it keeps what was accepted before and gets the last token -1. */
+gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, const void* target,
+                           const int32_t* d2t, const float* temperature, const float* u_node,
+                           const float* u_bonus, const gto_verdict* out, void* stream);
+
+/* Keeps the accepted nodes of every sequence: cache entry base + lead + path_node[s][j] is copied
+ * to base + lead + j for j < accept_len[s], in all layers, and kv_len_out[s] = base + lead +
+ * accept_len[s] (base + n for a sequence without a tree in this batch; untouched for one that is
+ * skipped).  kv_len_out must not be batch->kv_len, which the whole call reads.  path_node must
+ * increase along the path, as gto_verify_tree writes it. */
+gto_status gto_kv_commit(gto_decode_ctx* ctx, const gto_batch* batch, const gto_verdict* verdict,
+                         const gto_kv_cache* cache, int32_t* kv_len_out, void* stream);
+
+/* As gto_device_status and gto_launch_count, for a decoding context. */
+gto_status gto_decode_status(gto_decode_ctx* ctx, void* stream, int32_t* host_code);
+int64_t gto_decode_launch_count(const gto_decode_ctx* ctx);
 
 const char* gto_status_string(gto_status s);
 

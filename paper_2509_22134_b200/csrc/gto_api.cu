@@ -119,6 +119,7 @@ const char* gto_status_string(gto_status s) {
     case GTO_ERR_WORKSPACE: return "workspace allocation failed";
     case GTO_ERR_CUDA: return "CUDA runtime error";
     case GTO_ERR_NONFINITE: return "non-finite logit row";
+    case GTO_ERR_TIMEOUT: return "a wait inside a kernel ran out";
     case GTO_ERR_TOO_LARGE: return "batch exceeds the fixed scratch of the no-allocation call";
     case GTO_ERR_BAD_INDEX: return "an index in a caller's table was out of range";
   }

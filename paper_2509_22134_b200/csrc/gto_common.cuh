@@ -14,6 +14,7 @@ constexpr unsigned kFull = 0xffffffffu;
 // bits of the device status word
 constexpr int kStatusNonFinite = 1;
 constexpr int kStatusBadIndex = 4;  // an index read from a caller's table was out of range
+constexpr int kStatusTimeout = 8;   // a bounded wait ran out
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453094;
