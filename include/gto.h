@@ -379,7 +379,7 @@ typedef struct {
 
 /* Limits: 0 <= g <= 128; 1 <= D <= 16; n_q_heads a multiple of n_kv_heads, at most 128 of
  * them per key head; head_dim a multiple of 16, at most 256; rope_dims a multiple of 16, at
- * most head_dim; max_pages * page_size < 2^31; V * sizeof(logit) a multiple of 16 for the target
+ * most head_dim; max_pages * page_size <= 2^31 - 256; V * sizeof(logit) a multiple of 16 for the target
  * vocabulary and at most 1.5 MB; g <= V_draft <= V_target. */
 gto_status gto_decode_create(gto_decode_ctx** ctx, const gto_decode_config* cfg, int device);
 gto_status gto_decode_destroy(gto_decode_ctx* ctx);

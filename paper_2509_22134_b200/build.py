@@ -12,7 +12,7 @@ OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgto.so")
 SOURCES = ["gto_api.cu", "row_reduce.cu", "tree_build.cu", "tree_reward.cu", "surrogate_grad.cu",
            "build_tree_noalloc.cu", "token_loss.cu", "decode_api.cu", "kv_cache.cu", "tree_verify.cu",
-           "tree_attention_simt.cu"]
+           "tree_attention_simt.cu", "tree_attention_tc.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

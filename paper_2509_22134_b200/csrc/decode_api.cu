@@ -11,7 +11,9 @@ struct gto_decode_ctx {
   gto_decode_config cfg;
   int device;
   int sms;
+  char* ws;          // one allocation
   int32_t* status;
+  char* attn_ws;     // parts of blocks that were cut, null where the tensor-core kernel does not serve
   int64_t launches;
 };
 
@@ -126,7 +128,7 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
     if (c->n_q_heads / c->n_kv_heads > gto::kMaxGroup || c->head_dim % 16 || c->head_dim > gto::kMaxHeadDim ||
         c->rope_dims % 16 || c->n_kv_heads > 65535)
       return GTO_ERR_UNSUPPORTED;
-    if (static_cast<int64_t>(c->max_pages) * c->page_size >= (1ll << 31)) return GTO_ERR_UNSUPPORTED;
+    if (static_cast<int64_t>(c->max_pages) * c->page_size > (1ll << 31) - 256) return GTO_ERR_UNSUPPORTED;
     // work units of a call are counted in 32 bits
     if (static_cast<int64_t>(c->T) * c->n_q_heads + c->S >= (1ll << 30)) return GTO_ERR_UNSUPPORTED;
   }
@@ -154,16 +156,17 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
     delete ctx;
     return GTO_ERR_CUDA;
   }
-  void* ws = nullptr;
-  if (cudaMalloc(&ws, 256) != cudaSuccess) {
+  const bool tc = c->n_kv_heads > 0 && gto::attention_tc_serves(*c);
+  if (cudaMalloc(&ctx->ws, 256 + (tc ? gto::attention_tc_workspace(*c, ctx->sms) : 0)) != cudaSuccess) {
     cudaGetLastError();
     delete ctx;
     return GTO_ERR_WORKSPACE;
   }
-  ctx->status = static_cast<int32_t*>(ws);
-  if (cudaMemset(ws, 0, 256) != cudaSuccess) {
+  ctx->status = reinterpret_cast<int32_t*>(ctx->ws);
+  ctx->attn_ws = tc ? ctx->ws + 256 : nullptr;
+  if (cudaMemset(ctx->ws, 0, 256) != cudaSuccess) {
     cudaGetLastError();
-    cudaFree(ws);
+    cudaFree(ctx->ws);
     delete ctx;
     return GTO_ERR_WORKSPACE;
   }
@@ -174,7 +177,7 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
 gto_status gto_decode_destroy(gto_decode_ctx* ctx) {
   if (!ctx) return GTO_ERR_INVALID_ARG;
   DeviceGuard guard(ctx->device);
-  const cudaError_t e = cudaFree(ctx->status);
+  const cudaError_t e = cudaFree(ctx->ws);
   delete ctx;
   return e == cudaSuccess ? GTO_OK : GTO_ERR_CUDA;
 }
@@ -253,8 +256,14 @@ gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const
   a.scale = c.softmax_scale;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return GTO_ERR_CUDA;
-  if (gto::launch_attention_simt(a, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess)
-    return GTO_ERR_CUDA;
+  // a tensor map takes strides above 0 and below 2^40 bytes
+  const int64_t strides[6] = {a.c.k_page, a.c.k_entry, a.c.k_head, a.c.v_page, a.c.v_entry, a.c.v_head};
+  bool tc = ctx->attn_ws != nullptr;
+  for (int64_t x : strides) tc = tc && x > 0 && x < (1ll << 40);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  const cudaError_t err = tc ? gto::launch_attention_tc(a, ctx->attn_ws, ctx->sms, s, &ctx->launches)
+                           : gto::launch_attention_simt(a, s, &ctx->launches);
+  if (err != cudaSuccess) return GTO_ERR_CUDA;
   return GTO_OK;
 }
 

@@ -91,6 +91,11 @@ struct AttnArgs {
   int n_q_heads;
   float scale;
 };
+// Tensor-core kernel: whether it takes a configuration, what workspace it needs.
+bool attention_tc_serves(const gto_decode_config& c);
+size_t attention_tc_workspace(const gto_decode_config& c, int sms);
+cudaError_t launch_attention_tc(const AttnArgs& a, void* workspace, int sms, cudaStream_t stream,
+                                int64_t* launches);
 cudaError_t launch_attention_simt(const AttnArgs& a, cudaStream_t stream, int64_t* launches);
 
 }  // namespace gto

@@ -97,3 +97,31 @@ class Case:
                                      page_size=self.page, n_pages=self.n_pages, max_pages=self.max_pages, dtype=self.dtype,
                                      g=self.g, D=self.D, **kw)
         return gto.gto_decode_create(cfg, torch.device(self.device).index)
+
+    def attention_on_device(self, scale):
+        """What oracle.decode_oracle.attention gives, in fp64 on the device (for batches too long for its loops)."""
+        q, k, v = (torch.from_numpy(x).to(self.device) for x in (self.q, self.k, self.v))
+        out = torch.full((self.T, self.hq, self.dh), float("nan"), dtype=torch.float64, device=self.device)
+        spread, lse = out.clone(), out[:, :, 0].clone()
+        h = self.host
+        for s in range(self.S):
+            q0, q1, L = int(h["q_start"][s]), int(h["q_start"][s + 1]), int(h["kv_len"][s])
+            n = q1 - q0
+            if n == 0:
+                continue
+            nodes = 0 if not self.g else int(h["n_nodes"][s]) if "n_nodes" in h else self.g
+            e = torch.arange(L, device=self.device)
+            table = torch.from_numpy(h["page_table"][s]).to(self.device).long()
+            see = e[None] <= (L - n + torch.arange(n, device=self.device))[:, None]
+            if nodes:
+                see[n - nodes:, L - nodes:] = torch.from_numpy(h["node_mask"][s][:nodes, :nodes]).to(self.device)
+            rep = self.hq // self.hkv
+            kk = k[table[e // self.page], e % self.page].repeat_interleave(rep, 1).permute(1, 2, 0)
+            vv = v[table[e // self.page], e % self.page].repeat_interleave(rep, 1).permute(1, 0, 2)
+            x = (q[q0:q1].permute(1, 0, 2) @ kk * scale).masked_fill(~see, float("-inf"))
+            z = torch.logsumexp(x, 2)
+            w = torch.where(torch.isinf(z)[:, :, None], 0.0, torch.exp(x - z[:, :, None]))
+            out[q0:q1] = (w @ vv).permute(1, 0, 2)
+            spread[q0:q1] = (w @ vv.abs()).permute(1, 0, 2)
+            lse[q0:q1] = z.T
+        return out.cpu().numpy(), lse.cpu().numpy(), spread.cpu().numpy()

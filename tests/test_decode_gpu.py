@@ -94,8 +94,8 @@ def check_attention(gto, c, scale=None, lse=True, stream=None, ctx=None):
     compare_attention(c, scale, out, z)
 
 
-def compare_attention(c, scale, out, z):
-    want, want_z, spread = dec.attention(c.host, c.q, c.k, c.v, c.page, scale, c.g)
+def compare_attention(c, scale, out, z, want=None):
+    want, want_z, spread = want or dec.attention(c.host, c.q, c.k, c.v, c.page, scale, c.g)
     # a score is a sum of dh products in fp32, in any order: off by at most (dh + 2) 2^-23 sum |q k| scale (a tensor
     # core may cut instead of round, hence 2^-23), plus 2^-22 |score| for the exponential's argument; exp then errs by
     # twice that relative to itself in numerator and denominator.  A weight rounded to the type and the result rounded
@@ -209,6 +209,35 @@ def test_attention_reads_queries_out_of_a_projection(gto):
     gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, a)
     gto.gto_tree_attention(ctx, c.batch, qkv[:, :4], c.dk, c.dv, b)
     assert torch.equal(a, b)
+
+
+LONG = [
+    # sequences, tokens, longest cache, g, D: enough entries that every SM goes through several blocks of many tiles
+    (96, 1, 3000, 0, 1), (24, 61, 2500, 60, 7), (3, 900, 4000, 0, 1), (40, 2, 4500, 0, 1), (7, 130, 6000, 128, 9),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", [(8, 8, 64), (16, 4, 128)])
+@pytest.mark.parametrize("case", range(len(LONG)))
+def test_attention_long_batches(gto, case, shape, dtype):
+    """Ragged lengths; the result does not change from call to call, bit for bit."""
+    S, n, L, g, D = LONG[case]
+    hq, hkv, dh = shape
+    rng = np.random.default_rng(case)
+    q_lens = [n if g else int(rng.integers(1, n + 1)) for _ in range(S)]
+    kv_lens = [q + int(rng.integers(0, L)) for q in q_lens]
+    c = dc.Case(q_lens, kv_lens, hq, hkv, dh, [16, 64, 128, 8, 32][case], dtype, g, D, seed=case, scale=1.2)
+    ctx = c.ctx(gto)
+    out = torch.full((c.T, hq, dh), 5.0, dtype=c.dq.dtype, device=DEV)
+    z = torch.full((c.T, hq), 5.0, device=DEV)
+    gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=z)
+    again, z2 = torch.full_like(out, 5.0), torch.full_like(z, 5.0)
+    for _ in range(3):
+        gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, again, lse=z2)
+    assert gto.gto_decode_status(ctx) == 0
+    assert torch.equal(out, again) and torch.equal(z, z2)
+    compare_attention(c, dh ** -0.5, out, z, c.attention_on_device(dh ** -0.5))
 
 
 # ------------------------------------------------------------------ gto_verify_tree
