@@ -325,6 +325,26 @@ def test_verify_uniforms_at_their_ends(gto):
         assert out["token"][s, len(path)] == last
 
 
+@pytest.mark.parametrize("temperature", [1.0, 1e-3, 1e-30, 300.0])
+@pytest.mark.parametrize("S,V", [(3, 32000), (70, 4096)])
+def test_verify_flat_rows(gto, S, V, temperature):
+    """Rows whose tokens all weigh about the same: every border is nearer than fp32 sums can tell."""
+    rng = np.random.default_rng(V + S)
+    c = verify_case(rng, S, 6, 3, V, V, "f32")
+    c["target"] = np.round(rng.normal(size=c["target"].shape) * 0.05, 3)
+    c["target"] = dc.round_to(c["target"], "f32")
+    c["temperature"][:] = temperature
+    c["u_node"][:] = rng.random((S, 6)).astype(np.float32) * np.float32(3.0 / V)   # next to the children's probabilities
+    ctx, out = run_verify(gto, c, 3, V, V, "f32")
+    assert gto.gto_decode_status(ctx) == 0
+    for s in range(S):
+        path, ids, last, margin = dec.verify(c["parent"][s], c["token"][s], 1 + np.arange(6), c["target"][s], float(c["temperature"][s]),
+                                             c["u_node"][s].astype(float), float(c["u_bonus"][s]), 3)
+        if margin > 1e-13:
+            assert list(out["path_node"][s]) == path + [-1] * (3 - len(path))
+            assert list(out["token"][s]) == ids + [last] + [-1] * (3 - len(path))
+
+
 def test_verify_reports_rows_that_hold_no_distribution(gto):
     """NaN, +inf or nothing at all in a visited row; a bad temperature: reported, the sequence ends there."""
     c = verify_case(np.random.default_rng(3), 6, 12, 3, 512, 512, "f32")
