@@ -1,4 +1,5 @@
-"""ctypes binding of libgto.so: argument marshalling only.
+"""Binding of libgto.so: argument marshalling only, through ctypes, and through the extension _gto_decode
+for the calls of a decoding step, where microseconds count.
 
 The functions carry the names of the C entry points (include/gto.h) and take torch
 tensors for device buffers; PyTorch supplies device memory and streams, every step of
@@ -27,6 +28,11 @@ if not os.path.exists(LIB_PATH):
         f"{LIB_PATH} is missing: build it with `python -m paper_2509_22134_b200.build` "
         "(the GTO pass has no CPU or PyTorch fallback)")
 _lib = ctypes.CDLL(LIB_PATH)
+try:
+    from . import _gto_decode as _native
+except ImportError as e:
+    raise RuntimeError("_gto_decode.so is missing or does not fit this Python: build it with "
+                       "`python -m paper_2509_22134_b200.build`") from e
 
 
 class gto_config(ctypes.Structure):
@@ -129,22 +135,12 @@ class gto_verdict(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("accept_len", "path_node", "token")]
 
 
-_i64, _f32p = ctypes.c_int64, ctypes.c_void_p
 _lib.gto_decode_create.argtypes = [ctypes.POINTER(_vp), ctypes.POINTER(gto_decode_config), ctypes.c_int]
 _lib.gto_decode_destroy.argtypes = [_vp]
-_lib.gto_kv_append.argtypes = [_vp, ctypes.POINTER(gto_batch), ctypes.POINTER(gto_kv_cache), _vp, _i64, _vp, _i64,
-                               _vp, _i64, _vp, _vp, _vp, _vp, _vp]
-_lib.gto_tree_attention.argtypes = [_vp, ctypes.POINTER(gto_batch), ctypes.POINTER(gto_kv_cache), _vp, _i64, _vp,
-                                    _f32p, _vp]
-_lib.gto_verify_tree.argtypes = [_vp, ctypes.POINTER(gto_draft_tree), _vp, _vp, _vp, _vp, _vp,
-                                 ctypes.POINTER(gto_verdict), _vp]
-_lib.gto_kv_commit.argtypes = [_vp, ctypes.POINTER(gto_batch), ctypes.POINTER(gto_verdict),
-                               ctypes.POINTER(gto_kv_cache), _vp, _vp]
 _lib.gto_decode_status.argtypes = [_vp, _vp, ctypes.POINTER(ctypes.c_int32)]
 _lib.gto_decode_launch_count.argtypes = [_vp]
 _lib.gto_decode_launch_count.restype = ctypes.c_int64
-for _f in ("gto_decode_create", "gto_decode_destroy", "gto_kv_append", "gto_tree_attention", "gto_verify_tree",
-           "gto_kv_commit", "gto_decode_status"):
+for _f in ("gto_decode_create", "gto_decode_destroy", "gto_decode_status"):
     getattr(_lib, _f).restype = ctypes.c_int
 
 
@@ -354,7 +350,6 @@ def gto_kernel_times(ctx: int, stream=None) -> dict:
 
 _DTYPE_CODE = {torch.bfloat16: GTO_BF16, torch.float32: GTO_F32, torch.float16: GTO_F16,
                "bf16": GTO_BF16, "f32": GTO_F32, "f16": GTO_F16}
-_CODE_DTYPE = {GTO_BF16: torch.bfloat16, GTO_F32: torch.float32, GTO_F16: torch.float16}
 
 
 def make_decode_config(S, T=0, n_q_heads=0, n_kv_heads=0, head_dim=0, page_size=0, n_pages=0, max_pages=0,
@@ -375,20 +370,19 @@ class DecodeCtx:
     calls below check their tensors against.  gto_decode_destroy (or the end of the object) frees it."""
 
     def __init__(self, handle: int, cfg: gto_decode_config, device: int):
-        self.handle, self.cfg, self.device = handle, cfg, torch.device("cuda", device)
-        self.dtype = _CODE_DTYPE[cfg.kv_dtype]
-        self.logit_dtype = _CODE_DTYPE[cfg.logit_dtype]
+        self.handle, self.cfg, self.index = handle, cfg, device
+        self.native = _native.make(handle, bytes(cfg), device)
 
     def __del__(self):
         if self.handle and _lib is not None:
             _lib.gto_decode_destroy(self.handle)
-            self.handle = None
+            self.handle = self.native = None
 
 
 def _stream_of(ctx: DecodeCtx, stream) -> int:
     """The given stream, else the current one of the context's device (which need not be the current device)."""
     if stream is None:
-        return torch._C._cuda_getCurrentRawStream(ctx.device.index)
+        return torch._C._cuda_getCurrentRawStream(ctx.index)
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
@@ -399,96 +393,27 @@ def gto_decode_create(cfg: gto_decode_config, device: int = 0) -> DecodeCtx:
 
 
 def gto_decode_destroy(ctx: DecodeCtx):
-    handle, ctx.handle = ctx.handle, None
+    handle, ctx.handle, ctx.native = ctx.handle, None, None
     _check(_lib.gto_decode_destroy(handle), "gto_decode_destroy")
 
 
-def _ptr(ctx: DecodeCtx, t, name, dtype, shape):
-    """Device pointer of a dense tensor of the given type and shape on the context's device."""
-    if t.dtype != dtype or t.device != ctx.device or t.shape != shape or not t.is_contiguous():
-        raise ValueError(f"{name}: expected a contiguous {dtype} tensor of shape {tuple(shape)} on {ctx.device}, got "
-                         f"{t.dtype} {tuple(t.shape)} on {t.device}")
-    return t.data_ptr()
-
-
-def _rows(ctx: DecodeCtx, t, name, heads):
-    """(pointer, stride between tokens) of [T, heads, head_dim], the last two dimensions dense."""
-    c = ctx.cfg
-    if t.dtype != ctx.dtype or t.device != ctx.device or t.dim() != 3 or t.shape[1] != heads or \
-            t.shape[2] != c.head_dim or (t.shape[0] > 0 and (t.stride(2) != 1 or
-                                                             (heads > 1 and t.stride(1) != c.head_dim))):
-        raise ValueError(f"{name}: expected {ctx.dtype} [T, {heads}, {c.head_dim}] on {ctx.device} with dense heads, got "
-                         f"{t.dtype} {tuple(t.shape)} strides {t.stride()} on {t.device}")
-    return t.data_ptr(), (t.stride(0) if t.shape[0] > 1 else heads * c.head_dim)
-
-
-def _batch(ctx: DecodeCtx, batch: dict, T: int) -> gto_batch:
-    c = ctx.cfg
-    S = batch["kv_len"].shape[0]
-    i32 = torch.int32
-    b = gto_batch(S, T, _ptr(ctx, batch["q_start"], "q_start", i32, (S + 1,)),
-                  _ptr(ctx, batch["kv_len"], "kv_len", i32, (S,)),
-                  _ptr(ctx, batch["page_table"], "page_table", i32, (S, c.max_pages)))
-    t = batch.get("n_nodes")
-    if t is not None:
-        b.n_nodes = _ptr(ctx, t, "n_nodes", i32, (S,))
-    t = batch.get("node_mask")
-    if t is not None:
-        b.node_mask = _ptr(ctx, t, "node_mask", torch.int64, (S, c.g, (c.g + 63) // 64))
-    t = batch.get("node_depth")
-    if t is not None:
-        b.node_depth = _ptr(ctx, t, "node_depth", i32, (S, c.g))
-    return b
-
-
-def _cache(ctx: DecodeCtx, k, v, layers: bool = False) -> gto_kv_cache:
-    """Cache tensors [n_pages, page_size, n_kv_heads, head_dim], any strides with dense heads; with
-    `layers` also [n_layers, ...]."""
-    c = ctx.cfg
-    want = (c.n_pages, c.page_size, c.n_kv_heads, c.head_dim)
-    for t, name in ((k, "k_cache"), (v, "v_cache")):
-        if t.dtype != ctx.dtype or t.device != ctx.device or t.shape[-4:] != want or t.stride(-1) != 1 or \
-                t.dim() != 4 + (layers and t.dim() == 5) or t.shape != k.shape:
-            raise ValueError(f"{name}: expected {ctx.dtype} {'[n_layers], ' if layers else ''}{want} on {ctx.device} with "
-                             f"dense heads, got {t.dtype} {tuple(t.shape)} on {t.device}")
-    ks, vs = k.stride(), v.stride()
-    deep = k.dim() == 5
-    return gto_kv_cache(k.data_ptr(), v.data_ptr(), ks[-4], ks[-3], ks[-2], ks[0] if deep else 0,
-                        vs[-4], vs[-3], vs[-2], vs[0] if deep else 0, k.shape[0] if deep else 1)
-
+# Tensors that do not fit the context (type, shape, strides, device) raise ValueError.
 
 def gto_kv_append(ctx: DecodeCtx, batch: dict, q, k, v, q_out, k_cache, v_cache, inv_freq, q_norm=None, k_norm=None,
                   stream=None):
     """batch: dict of device tensors q_start [S+1], kv_len [S], page_table [S, max_pages] (int32) and, with trees,
-    node_mask (int64), node_depth, optionally n_nodes.  q and q_out may be None."""
-    c = ctx.cfg
-    kp, ks = _rows(ctx, k, "k", c.n_kv_heads)
-    vp, vs = _rows(ctx, v, "v", c.n_kv_heads)
-    T = k.shape[0]
-    if v.shape[0] != T or (q is not None and q.shape[0] != T):
-        raise ValueError("q, k and v must have the same number of tokens")
-    qp, qs, op = None, 0, None
-    if q is not None:
-        qp, qs = _rows(ctx, q, "q", c.n_q_heads)
-    if q_out is not None:
-        op = _ptr(ctx, q_out, "q_out", ctx.dtype, (T, c.n_q_heads, c.head_dim))
-    fp = None if inv_freq is None else _ptr(ctx, inv_freq, "inv_freq", torch.float64, (c.rope_dims // 2,))
-    qn = None if q_norm is None else _ptr(ctx, q_norm, "q_norm", ctx.dtype, (c.head_dim,))
-    kn = None if k_norm is None else _ptr(ctx, k_norm, "k_norm", ctx.dtype, (c.head_dim,))
-    b, kv = _batch(ctx, batch, T), _cache(ctx, k_cache, v_cache)
-    _check(_lib.gto_kv_append(ctx.handle, ctypes.byref(b), ctypes.byref(kv), qp, qs, kp, ks, vp, vs, op, fp, qn, kn,
-                              _stream_of(ctx, stream)), "gto_kv_append")
+    node_mask (int64), node_depth, optionally n_nodes.  q, k, v: [T, heads, head_dim], the last two dimensions dense;
+    q and q_out may be None.  k_cache, v_cache: [n_pages, page_size, n_kv_heads, head_dim], any strides with dense heads."""
+    code = _native.kv_append(ctx.native, batch, q, k, v, q_out, k_cache, v_cache, inv_freq, q_norm, k_norm,
+                             _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_kv_append")
 
 
 def gto_tree_attention(ctx: DecodeCtx, batch: dict, q, k_cache, v_cache, out, lse=None, stream=None):
-    c = ctx.cfg
-    qp, qs = _rows(ctx, q, "q", c.n_q_heads)
-    T = q.shape[0]
-    op = _ptr(ctx, out, "out", ctx.dtype, (T, c.n_q_heads, c.head_dim))
-    lp = None if lse is None else _ptr(ctx, lse, "lse", torch.float32, (T, c.n_q_heads))
-    b, kv = _batch(ctx, batch, T), _cache(ctx, k_cache, v_cache)
-    _check(_lib.gto_tree_attention(ctx.handle, ctypes.byref(b), ctypes.byref(kv), qp, qs, op, lp, _stream_of(ctx, stream)),
-           "gto_tree_attention")
+    code = _native.tree_attention(ctx.native, batch, q, k_cache, v_cache, out, lse, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_tree_attention")
 
 
 _VERDICT_FIELDS = ("accept_len", "path_node", "token")
@@ -500,43 +425,19 @@ def alloc_verdict(cfg: gto_decode_config, device, S=None) -> dict:
     return {n: torch.empty(shapes[n], dtype=torch.int32, device=device) for n in _VERDICT_FIELDS}
 
 
-def _verdict(ctx: DecodeCtx, v: dict, S: int) -> gto_verdict:
-    c, i32 = ctx.cfg, torch.int32
-    return gto_verdict(_ptr(ctx, v["accept_len"], "accept_len", i32, (S,)),
-                       _ptr(ctx, v["path_node"], "path_node", i32, (S, c.D)),
-                       _ptr(ctx, v["token"], "token", i32, (S, c.D + 1)))
-
-
 def gto_verify_tree(ctx: DecodeCtx, tree: dict, target, d2t, temperature, u_node, u_bonus, verdict: dict, stream=None):
     """tree: dict of [S, g] int32 tensors node_token and node_parent (with GTO_DECODE_CONTEXT_ROWS also node_depth and
     node_slot), optionally n_nodes [S]; target: [S, 1+g, V_target] or [S, R, V_target]."""
-    c, i32 = ctx.cfg, torch.int32
-    S = temperature.shape[0]
-    rows = 1 + (c.D - 1) * c.k if c.flags & GTO_DECODE_CONTEXT_ROWS else 1 + c.g
-    t = gto_draft_tree(S)
-    if c.g > 0:
-        for n in ("node_token", "node_parent") + (("node_depth", "node_slot") if c.flags & GTO_DECODE_CONTEXT_ROWS else ()):
-            setattr(t, n, _ptr(ctx, tree[n], n, i32, (S, c.g)))
-        if tree.get("n_nodes") is not None:
-            t.n_nodes = _ptr(ctx, tree["n_nodes"], "n_nodes", i32, (S,))
-    out = _verdict(ctx, verdict, S)
-    _check(_lib.gto_verify_tree(ctx.handle, ctypes.byref(t),
-                                _ptr(ctx, target, "target", ctx.logit_dtype, (S, rows, c.V_target)),
-                                None if d2t is None else _ptr(ctx, d2t, "d2t", i32, (c.V_draft,)),
-                                _ptr(ctx, temperature, "temperature", torch.float32, (S,)),
-                                None if u_node is None else _ptr(ctx, u_node, "u_node", torch.float32, (S, c.g)),
-                                _ptr(ctx, u_bonus, "u_bonus", torch.float32, (S,)), ctypes.byref(out),
-                                _stream_of(ctx, stream)), "gto_verify_tree")
+    code = _native.verify_tree(ctx.native, tree, target, d2t, temperature, u_node, u_bonus, verdict, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_verify_tree")
 
 
 def gto_kv_commit(ctx: DecodeCtx, batch: dict, verdict: dict, k_cache, v_cache, kv_len_out, stream=None):
     """k_cache, v_cache: [n_pages, ...] of one layer or [n_layers, n_pages, ...] of all."""
-    S = batch["kv_len"].shape[0]
-    b, kv = _batch(ctx, batch, ctx.cfg.T), _cache(ctx, k_cache, v_cache, layers=True)
-    out = _verdict(ctx, verdict, S)
-    _check(_lib.gto_kv_commit(ctx.handle, ctypes.byref(b), ctypes.byref(out), ctypes.byref(kv),
-                              _ptr(ctx, kv_len_out, "kv_len_out", torch.int32, (S,)), _stream_of(ctx, stream)),
-           "gto_kv_commit")
+    code = _native.kv_commit(ctx.native, batch, verdict, k_cache, v_cache, kv_len_out, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_kv_commit")
 
 
 def gto_decode_status(ctx: DecodeCtx, stream=None) -> int:

@@ -1,4 +1,5 @@
-"""Builds libgto.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds libgto.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a, and _gto_decode.so (the
+argument checks of the decoding-step calls, a Python extension beside it) with the host compiler."""
 from __future__ import annotations
 
 import os
@@ -10,6 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgto.so")
+EXT = os.path.join(HERE, "_gto_decode.so")
 SOURCES = ["gto_api.cu", "row_reduce.cu", "tree_build.cu", "tree_reward.cu", "surrogate_grad.cu",
            "build_tree_noalloc.cu", "token_loss.cu", "decode_api.cu", "kv_cache.cu", "tree_verify.cu",
            "tree_attention_simt.cu", "tree_attention_tc.cu"]
@@ -56,10 +58,23 @@ def build(force: bool = False, verbose: bool = False) -> str:
         list(ex.map(compile_one, jobs))
     objs = [os.path.join(OBJ, s.replace(".cu", ".o")) for s in SOURCES]
     if force or jobs or _stale(LIB, objs):
-        r = subprocess.run([_nvcc(), "-shared", "-o", LIB, *objs, "-cudart", "static", "-ldl"],
+        r = subprocess.run([_nvcc(), "-shared", "-Xlinker", "-soname=libgto.so", "-o", LIB, *objs, "-cudart", "static", "-ldl"],
                            capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stderr}")
+    src = os.path.join(CSRC, "decode_binding.cpp")
+    if force or _stale(EXT, [src, headers[-1]]):
+        import sysconfig
+        import torch
+        inc = os.path.join(os.path.dirname(torch.__file__), "include")
+        r = subprocess.run(["g++", "-O2", "-std=c++17", "-fPIC", "-shared", src, "-o", EXT, "-I", inc, "-I",
+                            os.path.join(inc, "torch", "csrc", "api", "include"), "-I",
+                            sysconfig.get_paths()["include"],
+                            f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                            LIB, "-Wl,-rpath,$ORIGIN", "-L", os.path.join(os.path.dirname(inc), "lib"),
+                            "-ltorch_python", "-ltorch_cpu", "-lc10"], capture_output=True, text=True)
+        if r.returncode != 0:
+            raise RuntimeError(f"g++ failed on {src}:\n{r.stderr}")
     return LIB
 
 
