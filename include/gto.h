@@ -16,7 +16,7 @@
  * multiple of 16 bytes.  All pointers in the structs below are DEVICE pointers owned by
  * the caller, 16-byte aligned, dense row-major with the shapes given.  The library
  * allocates memory only in gto_create (its device workspace and a page-locked host copy of
- * the row list for gto_tree_reward_host) and keeps no caller pointer
+ * the row list for gto_tree_reward_host) and gto_decode_create (its workspace) and keeps no caller pointer
  * after a call returns.  Calls enqueue work on `stream` (a cudaStream_t passed as void*)
  * and return without synchronising; argument errors are returned at once and launch
  * nothing.  Data faults (a non-finite row sum, an index out of range in a caller's table) are recorded
@@ -421,7 +421,9 @@ gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const
  * arg-max (lowest id on ties), and the last token is the arg-max.
  * target: [S, 1+g, V_target] (see GTO_DECODE_CONTEXT_ROWS); d2t: [V_draft] or NULL (identity,
  * needs V_draft == V_target); temperature, u_bonus: [S] fp32; u_node: [S, g] fp32; the uniforms
- * are given by the caller, in [0, 1) (clamped to it).  Sums are fp64.  A sequence whose visited
+ * are given by the caller, in [0, 1) (clamped to it).  The decisions are those of fp64 sums (a
+ * row is first summed in fp32 with a bound on its error, and again in fp64 where a decision lies
+ * within that bound of its border).  A sequence whose visited
  * rows hold NaN or +inf, or nothing but -inf, or whose temperature is negative or not finite,
  * is reported (GTO_ERR_NONFINITE); it keeps what was accepted before and gets the last token -1. */
 gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, const void* target,

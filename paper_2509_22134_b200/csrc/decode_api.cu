@@ -55,6 +55,9 @@ gto_status batch_args(const gto_decode_ctx* ctx, const gto_batch* in, bool needs
   const gto_decode_config& c = ctx->cfg;
   if (!in || in->S < 0 || in->T < 0) return GTO_ERR_INVALID_ARG;
   if (in->S > c.S || in->T > c.T || c.n_kv_heads == 0) return GTO_ERR_INVALID_ARG;
+  out->S = in->S;
+  out->T = in->T;
+  if (in->S == 0) return GTO_OK;  // its arrays have no elements and may have no address
   if (!table(in->q_start, 4) || !table(in->kv_len, 4) || !table(in->page_table, 4)) return GTO_ERR_INVALID_ARG;
   if (in->n_nodes && !aligned(in->n_nodes, 4)) return GTO_ERR_INVALID_ARG;
   if (in->node_mask && !aligned(in->node_mask, 8)) return GTO_ERR_INVALID_ARG;
@@ -65,8 +68,6 @@ gto_status batch_args(const gto_decode_ctx* ctx, const gto_batch* in, bool needs
   if (!tree && in->n_nodes) return GTO_ERR_INVALID_ARG;
   if (tree && needs_depth && !in->node_depth) return GTO_ERR_INVALID_ARG;
   if (tree && needs_mask && !in->node_mask) return GTO_ERR_INVALID_ARG;
-  out->S = in->S;
-  out->T = in->T;
   out->g = c.g;
   out->W = (c.g + 63) / 64;
   out->page_size = c.page_size;
@@ -164,7 +165,8 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
   }
   ctx->status = reinterpret_cast<int32_t*>(ctx->ws);
   ctx->attn_ws = tc ? ctx->ws + 256 : nullptr;
-  if (cudaMemset(ctx->ws, 0, 256) != cudaSuccess) {
+  // (waited for: the first call may come on a stream that the default one does not order)
+  if (cudaMemset(ctx->ws, 0, 256) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
     cudaGetLastError();
     cudaFree(ctx->ws);
     delete ctx;

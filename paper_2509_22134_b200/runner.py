@@ -1,6 +1,7 @@
-"""Convenience driver of one full pass (build tree -> reward -> surrogate gradient).
+"""Convenience drivers: one full training pass (build tree -> reward -> surrogate gradient), and the
+decoding step that a trained draft serves (append -> attention in every layer -> verify -> commit).
 
-Owns a library context and the caller-side buffers; every step is one C-ABI call.
+Each owns a library context and the caller-side buffers; every step is one C-ABI call.
 """
 from __future__ import annotations
 
@@ -88,3 +89,66 @@ class GtoPass:
 
     def launches(self) -> int:
         return gto.gto_launch_count(self.ctx)
+
+
+def draft_trees(tree: dict, b0: int = 0, b1: int | None = None, t: int = 0) -> dict:
+    """The decoding arrays of trees [b0, b1) that gto_build_tree made (t = 0: the current draft's), as views."""
+    return {n: tree[n][t, b0:b1] for n in ("node_token", "node_parent", "node_depth", "node_slot", "node_mask")}
+
+
+class DecodeStep:
+    """Decoding with draft trees: S sequences over a paged cache of n_layers layers.
+
+    A step is begin(), attend() for every layer, verify() and commit(); nothing waits for the device, and a
+    step can be captured into a CUDA graph.  kv_len holds the cached entries of every sequence; page_table
+    is the caller's to fill (a page may be added between steps).
+    """
+
+    def __init__(self, cfg: gto.gto_decode_config, n_layers: int, inv_freq, device="cuda:0"):
+        self.cfg, self.device = cfg, torch.device(device)
+        idx = self.device.index if self.device.index is not None else torch.cuda.current_device()
+        self.ctx = gto.gto_decode_create(cfg, idx)
+        dtype = {gto.GTO_BF16: torch.bfloat16, gto.GTO_F16: torch.float16,
+                 gto.GTO_F32: torch.float32}[cfg.kv_dtype]
+        pool = (n_layers, cfg.n_pages, cfg.page_size, cfg.n_kv_heads, cfg.head_dim)
+        self.k_cache = torch.zeros(pool, dtype=dtype, device=self.device)
+        self.v_cache = torch.zeros(pool, dtype=dtype, device=self.device)
+        self.page_table = torch.full((cfg.S, cfg.max_pages), -1, dtype=torch.int32, device=self.device)
+        self.kv_len = torch.zeros(cfg.S, dtype=torch.int32, device=self.device)
+        self.inv_freq = torch.as_tensor(inv_freq, dtype=torch.float64, device=self.device)
+        self.verdict = gto.alloc_verdict(cfg, self.device)
+        self.q_rotated = torch.empty((cfg.T, cfg.n_q_heads, cfg.head_dim), dtype=dtype, device=self.device)
+        self.batch = None
+
+    def close(self):
+        if self.ctx is not None:
+            gto.gto_decode_destroy(self.ctx)
+            self.ctx = None
+
+    def begin(self, q_start, trees: dict | None = None):
+        """The tokens of this step: chunk s is q_start[s] .. q_start[s+1], what comes before the draft tree (a
+        prompt, or the last step's token) and then the tree's nodes."""
+        self.batch = {"q_start": q_start, "kv_len": self.kv_len + torch.diff(q_start), "page_table": self.page_table}
+        if trees is not None:
+            self.batch.update({n: trees[n] for n in ("node_mask", "node_depth", "n_nodes") if n in trees})
+
+    def attend(self, layer: int, q, k, v, out, lse=None, q_norm=None, k_norm=None, stream=None):
+        """Keys and values of one layer into its cache, then the attention of the step's tokens over it."""
+        rotated = self.q_rotated[:q.shape[0]]
+        gto.gto_kv_append(self.ctx, self.batch, q, k, v, rotated, self.k_cache[layer], self.v_cache[layer],
+                          self.inv_freq, q_norm, k_norm, stream)
+        gto.gto_tree_attention(self.ctx, self.batch, rotated, self.k_cache[layer], self.v_cache[layer], out, lse, stream)
+
+    def verify(self, trees: dict, target, d2t, temperature, u_node, u_bonus, stream=None) -> dict:
+        gto.gto_verify_tree(self.ctx, trees, target, d2t, temperature, u_node, u_bonus, self.verdict, stream)
+        return self.verdict
+
+    def commit(self, stream=None):
+        """Keeps the accepted nodes' entries in all layers; kv_len then counts them."""
+        gto.gto_kv_commit(self.ctx, self.batch, self.verdict, self.k_cache, self.v_cache, self.kv_len, stream)
+
+    def status(self) -> int:
+        return gto.gto_decode_status(self.ctx)
+
+    def launches(self) -> int:
+        return gto.gto_decode_launch_count(self.ctx)
