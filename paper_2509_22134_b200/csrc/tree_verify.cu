@@ -1,17 +1,25 @@
 // gto_verify_tree: the walk of a drafted tree against the target's probabilities.
 //
-// One thread-block cluster of eight (or four) CTAs per sequence.  At every context it visits, the CTAs
-// stream their shares of the target row into shared memory once, exchange (maximum, sum) through
-// distributed shared memory, and every CTA makes the same decisions about the children from the
-// same numbers; where the walk ends, the CTA whose range the random number falls into finds the
-// token from its shared copy.  A row that is not visited is not read.
+// One thread-block cluster of eight CTAs per sequence.  At every context it visits, the CTAs go
+// through their shares of the target row once (seven warps, each with a range of its own, so that a
+// last token is looked for in one warp's range only), exchange (reference, sum) through distributed
+// shared memory, and an eighth warp of every CTA makes the same decisions about the children from
+// the same numbers.  Where the walk ends, the CTA whose range the random number falls into reads that
+// range again and finds the token.  A row that is not visited is not read.
 //
 // Results are those of fp64 arithmetic: the token drawn from a vocabulary of 10^5 ids is decided by a
 // cumulative sum, and with fp32 terms about one draw in a hundred from a flat distribution would fall
 // to rounding.  But fp64 exponentials of all weights took 190 us where the row's bytes take 20
 // (128 trees, 128 256 ids), so that every row is first summed with fp32 exponentials, and decisions
 // are taken only where they are further from their border than the sum can be wrong (kSlack); a
-// row where one is not is summed again in fp64, from shared memory.
+// row where one is not is summed again in fp64.
+//
+// What bounds it is the chain: a sequence's rows come one after another, 8 of them for the longest
+// walk of the 128, and a row is a load's latency (0.8 us), a thread's 72 to 144 weights (1.5 to 4 us,
+// depending on how many CTAs share the SM), the exchange (1.2 us) and the decision (1 us); a draw from
+// the flat tail then costs the row in fp64 (4 us alone, 15 us when all sequences do).  Measured: one
+// tree of 32 000 ids 13.2 us, 128 trees of 128 256 ids 84 us (103 us with the row kept in shared
+// memory, which left room for three quarters of the clusters and took a second pass for the weights).
 #include <cooperative_groups.h>
 
 #include "decode_common.cuh"
@@ -21,14 +29,25 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int kMaxCluster = 8;
-constexpr int kWarps = 8;                    // that share the row
+constexpr int kCluster = 8;                  // CTAs of a sequence
+constexpr int kWarps = 7;                    // that share the row
+constexpr int kWidth = 8;                    // lanes that their sums take
 constexpr int kThreads = (kWarps + 1) * 32;  // and one that knows the tree and decides
 
+// A thread's vectors of a row come through shared memory, kBatch at a time, kGroups batches on their way.
+constexpr int kRowThreads = kWarps * 32;
+constexpr int kBatch = 3, kGroups = 4;
+constexpr int kStageBytes = kBatch * kGroups * kRowThreads * 16;
+static_assert(((kMaxTargetRow / 16 / kCluster + 1) / kWarps + 1) * 16 <= kStageBytes, "a warp's range fits");
+
+// How far a thread's reference may lie below its largest logit, in log2 units: rescaling for every new
+// maximum took longer than the weights.
+constexpr float kReach = 4.f;
+
 // How far a sum of fp32 weights can be from the true one, relative to the row's whole mass.  A weight
-// 2^-a is off by 2^-22 (the exponential) and 3 * 2^-24 * a * ln 2 (roundings of its argument)
-// relative to itself; the mean of a over the distribution is at most log2 V <= 19.6; eight weights are
-// added in fp32, the rest in fp64.  In all below 3.2e-6.
+// 2^-a is off by 2^-22 (the exponential) and 3 * 2^-24 * (a + kReach) * ln 2 (roundings of its argument)
+// relative to itself; the mean of a over the distribution is at most log2 V <= 19.6; 24 weights are
+// added in fp32, in five levels (5 * 2^-24), the rest in fp64.  In all below 3.5e-6.
 constexpr double kSlack = 4e-6;
 
 struct Part {
@@ -43,18 +62,18 @@ __device__ __forceinline__ double sum64(double v) {
   return v;
 }
 
-// Sum of the first kWidth lanes, for all lanes.
-template <int kWidth>
+// Sum of the first kLanes lanes, for all lanes.
+template <int kLanes>
 __device__ __forceinline__ double sum_first(double v) {
 #pragma unroll
-  for (int o = kWidth / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
+  for (int o = kLanes / 2; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
   return __shfl_sync(kFull, v, 0);
 }
-// Inclusive sums over the lanes, up to `width` of them.
-template <int kWidth>
+// Inclusive sums over the lanes, up to kLanes of them.
+template <int kLanes>
 __device__ __forceinline__ double scan64(double v, int lane) {
 #pragma unroll
-  for (int o = 1; o < kWidth; o <<= 1) {
+  for (int o = 1; o < kLanes; o <<= 1) {
     const double y = __shfl_up_sync(kFull, v, o);
     if (lane >= o) v += y;
   }
@@ -83,17 +102,52 @@ __device__ __forceinline__ double exp2_neg(double x) {
   return x < -1000.0 ? 0.0 : r;
 }
 
-// Whether 16 bytes of logits hold a NaN.
+// The largest of 16 bytes of logits, of two packed 16-bit ones at a time; NaN if one of them is.
 template <typename T>
-__device__ __forceinline__ bool has_nan(const uint4& v) {
-  if (T::kBytes == 4) {
-    const auto nan = [](uint32_t w) { return (w & 0x7fffffffu) > 0x7f800000u; };
-    return nan(v.x) || nan(v.y) || nan(v.z) || nan(v.w);
+__device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
+  uint32_t d;
+  if (T::kBytes == 4) asm("max.NaN.f32 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  else if (T::kNegInfElem == 0xff80u) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
+  return d;
+}
+template <typename T>
+__device__ __forceinline__ uint32_t max_of(const uint4& v) {
+  return max_word<T>(max_word<T>(v.x, v.y), max_word<T>(v.z, v.w));
+}
+template <typename T>
+__device__ __forceinline__ float max_half(uint32_t w) {  // of the word's two halves
+  if (T::kBytes == 4) return __uint_as_float(w);
+  w = max_word<T>(w, __byte_perm(w, w, 0x1032));
+  return T::load1(&w, 0);
+}
+
+// Sum of the weights of 16 bytes of logits, 2^((f - m) c2), in fp32: pairs side by side.
+template <typename T>
+__device__ __forceinline__ float weights(const uint4& v, float m, float c2) {
+  constexpr int E = T::kPerVec;
+  float f[E];
+  T::unpack(v, f);
+  uint64_t neg, scale, sum[E / 2];
+  asm("mov.b64 %0, {%1, %1};" : "=l"(neg) : "f"(-m));
+  asm("mov.b64 %0, {%1, %1};" : "=l"(scale) : "f"(c2));
+#pragma unroll
+  for (int e = 0; e < E / 2; ++e) {
+    float a, b;
+    asm("{\n .reg .b64 x;\n mov.b64 x, {%2, %3};\n add.rn.f32x2 x, x, %4;\n mul.rn.f32x2 x, x, %5;\n mov.b64 {%0, %1}, x;\n}"
+        : "=f"(a), "=f"(b)
+        : "f"(f[2 * e]), "f"(f[2 * e + 1]), "l"(neg), "l"(scale));
+    a = ex2_approx(a);
+    b = ex2_approx(b);
+    asm("mov.b64 %0, {%1, %2};" : "=l"(sum[e]) : "f"(a), "f"(b));
   }
-  // an absolute value above that of infinity carries into the sign
-  constexpr uint32_t kInf = static_cast<uint32_t>(T::kNegInfElem) & 0x7fffu, kAdd = (0x7fffu - kInf) * 0x10001u;
-  const auto nan = [](uint32_t w) { return (w & 0x7fff7fffu) + kAdd; };
-  return ((nan(v.x) | nan(v.y) | nan(v.z) | nan(v.w)) & 0x80008000u) != 0;
+#pragma unroll
+  for (int w = E / 4; w > 0; w /= 2)
+#pragma unroll
+    for (int e = 0; e < w; ++e) asm("add.rn.f32x2 %0, %1, %2;" : "=l"(sum[e]) : "l"(sum[e]), "l"(sum[e + w]));
+  float a, b;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(sum[0]));
+  return a + b;
 }
 
 // A 4- or 8-byte value into the same place of another CTA's shared memory.
@@ -102,12 +156,11 @@ __device__ __forceinline__ void push(cg::cluster_group& cluster, V* place, int t
   *cluster.map_shared_rank(place, to) = value;
 }
 
-template <typename T, int kCluster>
-__global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) verify_tree_kernel(VerifyArgs a) {
+template <typename T, int kResident>
+__global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(VerifyArgs a) {
   constexpr int E = T::kPerVec;
-  constexpr int U = kCluster == kMaxCluster ? 8 : 4;  // vectors in flight per thread
   constexpr int kChunks = kMaxNodes / 32;
-  extern __shared__ __align__(16) unsigned char s_raw[];  // the CTA's share of the row
+  extern __shared__ __align__(16) unsigned char s_raw[];  // vectors on their way; a warp's range, where the last token is
   __shared__ Part s_part[2][kCluster];  // what the CTAs say of a row, sent by each to all
   __shared__ int s_redo;                // sent by the owner of the last token
   __shared__ double s_wsum[kWarps];
@@ -118,7 +171,7 @@ __global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) ver
   __shared__ double s_p[kMaxNodes];                      // and their weights
   __shared__ int s_child, s_owner, s_close;
   __shared__ double s_run[kWarps * 32];                  // sums of runs of vectors
-  __shared__ int s_from;
+  __shared__ int s_from, s_out;
   __shared__ float s_top;
 
   cg::cluster_group cluster = cg::this_cluster();
@@ -168,9 +221,37 @@ __global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) ver
     if (report) atomicOr(a.status, kStatusBadIndex);
   }
 
+  // The warp's range of a row, for the row warps: take(x, i) with x the vectors i, i + 32, ... below w1.  A
+  // thread waits only for what it copied itself.
+  const auto fetch = [&](const char* z, int b) {
+#pragma unroll
+    for (int u = 0; u < kBatch; ++u) {
+      const int i = w0 + lane + 32 * (b * kBatch + u);
+      if (i < w1)
+        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(static_cast<uint32_t>(
+                         __cvta_generic_to_shared(s_vec + ((b % kGroups) * kBatch + u) * kRowThreads + tid))),
+                     "l"(z + static_cast<int64_t>(vec0 + i) * 16)
+                     : "memory");
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+  };
+  const auto stream = [&](const char* z, auto&& take) {
+#pragma unroll
+    for (int b = 0; b < kGroups; ++b) fetch(z, b);
+#pragma unroll 1
+    for (int b = 0; w0 + 32 * kBatch * b < w1; ++b) {
+      asm volatile("cp.async.wait_group %0;" ::"n"(kGroups - 1) : "memory");
+      uint4 x[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) x[u] = s_vec[((b % kGroups) * kBatch + u) * kRowThreads + tid];
+      take(x, w0 + lane + 32 * kBatch * b);
+      fetch(z, b + kGroups);
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+  };
+
   int cur = -1, row = 0, len = 0, bonus = -1;
-  bool exact = false;  // the row is in shared memory and is summed again, in fp64
-  float m_warp = -INFINITY;
+  bool exact = false;  // the row is summed again, in fp64
   for (int step = 0; cold_ok; ++step) {
     const bool ex = exact || !(c2 < 1e30f);  // (a temperature next to 0 is beyond fp32)
     const char* z = a.target + (static_cast<int64_t>(s) * a.rows + row) * a.V_target * T::kBytes;
@@ -186,94 +267,115 @@ __global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) ver
         }
       }
     } else if (!exact) {
-      // ---- the row's share: shared memory, maximum, soundness
-      typename T::MaxAcc acc = T::max_init();
+      // ---- the row's share in one pass: a thread's weights are relative to about the largest logit that
+      // it has met (what it had is rescaled in fp64, which costs the sum nothing)
+      float m = -INFINITY;
+      double sum = 0.0;
       bool bad = false;
-      for (int i = w0 + lane; i < w1; i += 32 * U) {
-        uint4 x[U];
+      uint4 best[kBatch] = {};  // greedy: the first batch that had the maximum
+      int best_i = w1;
+      const float reach = kReach / c2;
+      stream(z, [&](const uint4 (&x)[kBatch], int i) {
+        uint32_t word = T::kNegInfWord;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (i + 32 * u < w1) x[u] = ld_stream16(z + static_cast<int64_t>(vec0 + i + 32 * u) * 16);
+        for (int u = 0; u < kBatch; ++u)
+          if (i + 32 * u < w1) word = max_word<T>(word, max_of<T>(x[u]));
+        const float top = max_half<T>(word);
+        bad |= top != top;
+        if (greedy || ex) {
+          if (top > m) {
+            m = top;
+            best_i = i;
 #pragma unroll
-        for (int u = 0; u < U; ++u)
-          if (i + 32 * u < w1) {
-            s_vec[i + 32 * u] = x[u];
-            T::max_update(acc, x[u]);
-            bad |= has_nan<T>(x[u]);
+            for (int u = 0; u < kBatch; ++u) best[u] = x[u];
           }
-      }
-      m_warp = warp_max_f32(T::max_value(acc));
+          return;
+        }
+        if (m == -INFINITY ? top > m : top > m + reach) {
+          if (sum != 0.0) sum *= exp2_neg((static_cast<double>(m) - static_cast<double>(top)) * c64);
+          m = top;
+        }
+        if (m == -INFINITY) return;
+        float part[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          part[u] = 0.f;
+          if (i + 32 * u < w1) part[u] = weights<T>(x[u], m, c2);
+        }
+        sum += static_cast<double>((part[0] + part[1]) + part[2]);
+      });
+      const float m_warp = warp_max_f32(m);
+      if (sum != 0.0) sum *= exp2_neg((static_cast<double>(m) - static_cast<double>(m_warp)) * c64);
+      sum = sum64(sum);
       bad = __any_sync(kFull, bad);
       if (lane == 0) {
         s_wmax[warp] = m_warp;
         s_wbad[warp] = bad;
+        s_wsum[warp] = sum;
+      }
+      if (greedy) {
+        // the lowest id of the warp's range that has its maximum
+        int at = 0x7fffffff;
+#pragma unroll
+        for (int u = kBatch - 1; u >= 0; --u) {
+          float f[E];
+          T::unpack(best[u], f);
+#pragma unroll
+          for (int e = E - 1; e >= 0; --e)
+            if (f[e] == m_warp && best_i + 32 * u < w1) at = (vec0 + best_i + 32 * u) * E + e;
+        }
+        at = __reduce_min_sync(kFull, at);
+        if (lane == 0) s_wid[warp] = at;
       }
     }
     __syncthreads();
     float m_cta = s_wmax[0];
-    int any_bad = s_wbad[0];
 #pragma unroll
-    for (int w = 1; w < kWarps; ++w) {
-      m_cta = fmaxf(m_cta, s_wmax[w]);
-      any_bad |= s_wbad[w];
-    }
-    if (!control) {
-      if (greedy) {
-        // the lowest id of the share that has its maximum
-        int at = 0x7fffffff;
-        for (int i = w0 + lane; i < w1 && m_warp == m_cta; i += 32) {
-          float f[E];
-          T::unpack(s_vec[i], f);
-#pragma unroll
-          for (int e = E - 1; e >= 0; --e)
-            if (f[e] == m_cta) at = min(at, (vec0 + i) * E + e);
-        }
-        at = __reduce_min_sync(kFull, at);
-        if (lane == 0) s_wid[warp] = at;
-      } else {
-        // ---- the share's sum, relative to its own maximum
+    for (int w = 1; w < kWarps; ++w) m_cta = fmaxf(m_cta, s_wmax[w]);
+    if (ex && !greedy) {  // the sums once more (or for the first time), in fp64
+      if (!control) {
         double sum = 0.0;
         if (m_cta != -INFINITY) {
-          if (ex) {
-            for (int i = w0 + lane; i < w1; i += 32) {
+          stream(z, [&](const uint4 (&x)[kBatch], int i) {
+#pragma unroll 1
+            for (int u = 0; u < kBatch; ++u) {
+              if (i + 32 * u >= w1) break;
               float f[E];
-              T::unpack(s_vec[i], f);
+              T::unpack(u == 0 ? x[0] : u == 1 ? x[1] : x[2], f);
 #pragma unroll
-              for (int e = 0; e < E; ++e)
-                sum += exp2_neg((static_cast<double>(f[e]) - static_cast<double>(m_cta)) * c64);
+              for (int e = 0; e < E; ++e) sum += exp2_neg((static_cast<double>(f[e]) - static_cast<double>(m_cta)) * c64);
             }
-          } else {
-            for (int i = w0 + lane; i < w1; i += 32) {
-              float f[E];
-              T::unpack(s_vec[i], f);
-              float part = 0.f;
-#pragma unroll
-              for (int e = 0; e < E; ++e) part += ex2_approx((f[e] - m_cta) * c2);
-              sum += static_cast<double>(part);
-            }
-          }
+          });
         }
         sum = sum64(sum);
         if (lane == 0) s_wsum[warp] = sum;
       }
+      __syncthreads();
     }
-    __syncthreads();
     if (!joined) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
     joined = true;
-    if (tid < kCluster) {  // one thread for each CTA that hears it
-      double sum = 0.0;
-      int at = 0;
-      if (greedy) {
-        at = s_wid[0];
-        for (int w = 1; w < kWarps; ++w) at = min(at, s_wid[w]);
-        if (at == 0x7fffffff) at = 0;
-      } else {
-        for (int w = 0; w < kWarps; ++w) sum += s_wsum[w];
+    double warp_sum = 0.0;  // the control warp's lane w: the sum of warp w's range, relative to the CTA's maximum
+    if (control) {
+      int at = 0x7fffffff, wrong = 0;
+      if (lane < kWarps) {
+        wrong = s_wbad[lane];
+        if (greedy) {
+          if (s_wmax[lane] == m_cta) at = s_wid[lane];
+        } else {
+          warp_sum = s_wsum[lane];
+          if (!ex && warp_sum != 0.0)
+            warp_sum *= exp2_neg((static_cast<double>(s_wmax[lane]) - static_cast<double>(m_cta)) * c64);
+        }
       }
-      Part* mine = &s_part[step & 1][rank];
-      push(cluster, &mine->sum, tid, sum);
-      push(cluster, &mine->best, tid, make_key(m_cta, at));
-      push(cluster, &mine->bad, tid, any_bad);
+      at = __reduce_min_sync(kFull, at);
+      wrong = __any_sync(kFull, wrong);
+      const double sum = sum_first<kWidth>(warp_sum);
+      if (lane < kCluster) {  // one thread for each CTA that hears it
+        Part* mine = &s_part[step & 1][rank];
+        push(cluster, &mine->sum, lane, sum);
+        push(cluster, &mine->best, lane, make_key(m_cta, at == 0x7fffffff ? 0 : at));
+        push(cluster, &mine->bad, lane, wrong);
+      }
     }
     cluster.sync();
     // ---- the control warp of every CTA: the row's maximum and sum, and the children
@@ -419,47 +521,45 @@ __global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) ver
       double before = 0.0;
       if (control) {
         // what is left of the warps' ranges; the one that holds the token is the last that begins at or below aim
-        double rest = lane < kWarps ? s_wsum[lane] * scale : 0.0;
+        double rest = warp_sum * scale;
         if (lane < kWarps) {
           const int lo = (vec0 + min(lane * per_warp, vecs)) * E, hi = (vec0 + min((lane + 1) * per_warp, vecs)) * E;
           for (int r = 0; r < removed; ++r)
             if (s_removed[r] >= lo && s_removed[r] < hi) rest -= s_p[r];
           rest = fmax(rest, 0.0);
         }
-        const double upto = scan64<kWarps>(rest, lane);
-        const unsigned some = __ballot_sync(kFull, rest > 0.0) & 0xffu;
-        const unsigned below = __ballot_sync(kFull, rest > 0.0 && before_cta + (upto - rest) <= aim) & 0xffu;
+        const double upto = scan64<kWidth>(rest, lane);
+        const unsigned some = __ballot_sync(kFull, rest > 0.0) & ((1u << kWarps) - 1);
+        const unsigned below = __ballot_sync(kFull, rest > 0.0 && before_cta + (upto - rest) <= aim) & ((1u << kWarps) - 1);
         const int from = below != 0 ? 31 - __clz(below) : some != 0 ? __ffs(some) - 1 : 0;
         before = before_cta + __shfl_sync(kFull, upto - rest, from);
-        // refused tokens leave the share
-        for (int r = lane; r < removed; r += 32) {
-          const int off = s_removed[r] - vec0 * E;
-          if (off >= 0 && off < vecs * E) reinterpret_cast<Elem*>(s_raw)[off] = T::kNegInfElem;
-        }
         if (lane == 0) {
           s_from = from;
+          s_out = removed;
           s_top = M;
         }
       }
       __syncthreads();
-      // all row warps: a thread sums a run of that range's vectors
+      // all row warps: a thread sums a run of that range's vectors, read again
       const int i0 = min(s_from * per_warp, vecs), i1 = min(i0 + per_warp, vecs);
       const int run = (i1 - i0 + kWarps * 32 - 1) / (kWarps * 32);
       const float top = s_top;
       if (!control) {
         const int r0 = min(i0 + tid * run, i1), r1 = min(r0 + run, i1);
+        for (int i = r0; i < r1; ++i) s_vec[i - i0] = ld_stream16(z + static_cast<int64_t>(vec0 + i) * 16);
+        for (int r = 0; r < s_out; ++r) {  // refused tokens have nothing left
+          const int off = s_removed[r] - vec0 * E;
+          if (off >= r0 * E && off < r1 * E) reinterpret_cast<Elem*>(s_raw)[off - i0 * E] = T::kNegInfElem;
+        }
         double sum = 0.0;
         for (int i = r0; i < r1; ++i) {
           float f[E];
-          T::unpack(s_vec[i], f);
+          T::unpack(s_vec[i - i0], f);
           if (ex) {
 #pragma unroll
             for (int e = 0; e < E; ++e) sum += exp2_neg((static_cast<double>(f[e]) - static_cast<double>(top)) * c64);
           } else {
-            float part = 0.f;
-#pragma unroll
-            for (int e = 0; e < E; ++e) part += ex2_approx((f[e] - top) * c2);
-            sum += static_cast<double>(part);
+            sum += static_cast<double>(weights<T>(s_vec[i - i0], top, c2));
           }
         }
         s_run[tid] = sum;
@@ -500,7 +600,7 @@ __global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) ver
         for (int e0 = 0; e0 < ids && found < 0; e0 += 32) {
           double wv = 0.0;
           if (e0 + lane < ids) {
-            const float f = T::load1(s_raw, v0 * E + e0 + lane);
+            const float f = T::load1(s_raw, (v0 - i0) * E + e0 + lane);
             wv = ex ? exp2_neg((static_cast<double>(f) - static_cast<double>(top)) * c64)
                     : static_cast<double>(ex2_approx((f - top) * c2));
           }
@@ -523,15 +623,6 @@ __global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) ver
     }
     cluster.sync();  // the owner's answer
     if (!ex && s_redo) {
-      // the owner took the refused tokens out of its share: put them back
-      if (rank == owner && control) {
-        for (int r = lane; r < removed; r += 32) {
-          const int off = s_removed[r] - vec0 * E;
-          if (off >= 0 && off < vecs * E)
-            reinterpret_cast<Elem*>(s_raw)[off] = reinterpret_cast<const Elem*>(z)[s_removed[r]];
-        }
-      }
-      __syncthreads();
       exact = true;
       continue;
     }
@@ -551,19 +642,12 @@ __global__ void __launch_bounds__(kThreads, kCluster == kMaxCluster ? 2 : 3) ver
   }
 }
 
-template <typename T, int kCluster>
+template <typename T, int kResident>
 cudaError_t verify_as(const VerifyArgs& a, cudaStream_t stream) {
-  const int nvec = a.V_target / T::kPerVec;
-  const size_t smem = static_cast<size_t>((nvec + kCluster - 1) / kCluster) * 16;
-  if (smem > 48 * 1024) {
-    const cudaError_t e = cudaFuncSetAttribute(verify_tree_kernel<T, kCluster>,
-                                               cudaFuncAttributeMaxDynamicSharedMemorySize, static_cast<int>(smem));
-    if (e != cudaSuccess) return e;
-  }
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(a.S) * kCluster);
   cfg.blockDim = dim3(kThreads);
-  cfg.dynamicSmemBytes = smem;
+  cfg.dynamicSmemBytes = kStageBytes;
   cfg.stream = stream;
   cudaLaunchAttribute attr{};
   attr.id = cudaLaunchAttributeClusterDimension;
@@ -572,16 +656,16 @@ cudaError_t verify_as(const VerifyArgs& a, cudaStream_t stream) {
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, verify_tree_kernel<T, kCluster>, a);
+  return cudaLaunchKernelEx(&cfg, verify_tree_kernel<T, kResident>, a);
 }
 
 template <typename T>
 cudaError_t verify_as(const VerifyArgs& a, int sms, cudaStream_t stream) {
-  // Eight CTAs a sequence give the shortest walk; where the sequences do not fit the device at three
-  // CTAs an SM, four, as long as three shares of a row fit an SM.
-  const size_t row = static_cast<size_t>(a.V_target) * T::kBytes;
-  const bool many = static_cast<int64_t>(a.S) * kMaxCluster > 3ll * sms && row / 4 <= 70 * 1024;
-  return many ? verify_as<T, kMaxCluster / 2>(a, stream) : verify_as<T, kMaxCluster>(a, stream);
+  // Two CTAs an SM may have 128 registers a thread: one tree of 32 000 ids took 13.2 us against 14.1 with
+  // 64.  Where the sequences do not fit the device so, four: 128 trees of 128 256 ids took 84 us against
+  // 97 at three an SM (and 91 in clusters of four CTAs, four an SM).
+  const bool few = static_cast<int64_t>(a.S) * kCluster <= 2ll * sms;
+  return few ? verify_as<T, 2>(a, stream) : verify_as<T, 4>(a, stream);
 }
 
 }  // namespace
