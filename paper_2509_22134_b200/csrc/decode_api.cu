@@ -264,7 +264,7 @@ gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const
   for (int64_t x : strides) tc = tc && x > 0 && x < (1ll << 40);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const cudaError_t err = tc ? gto::launch_attention_tc(a, ctx->attn_ws, ctx->sms, s, &ctx->launches)
-                           : gto::launch_attention_simt(a, s, &ctx->launches);
+                           : gto::launch_attention_simt(a, ctx->sms, s, &ctx->launches);
   if (err != cudaSuccess) return GTO_ERR_CUDA;
   return GTO_OK;
 }

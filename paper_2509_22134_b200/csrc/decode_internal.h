@@ -96,6 +96,6 @@ bool attention_tc_serves(const gto_decode_config& c);
 size_t attention_tc_workspace(const gto_decode_config& c, int sms);
 cudaError_t launch_attention_tc(const AttnArgs& a, void* workspace, int sms, cudaStream_t stream,
                                 int64_t* launches);
-cudaError_t launch_attention_simt(const AttnArgs& a, cudaStream_t stream, int64_t* launches);
+cudaError_t launch_attention_simt(const AttnArgs& a, int sms, cudaStream_t stream, int64_t* launches);
 
 }  // namespace gto

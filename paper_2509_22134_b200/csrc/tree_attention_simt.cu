@@ -3,10 +3,13 @@
 //
 // Online softmax over tiles of 32 cache entries.  A CTA owns 16 query rows of one key head (a row is
 // one token and one of the query heads that share the key head), so that a tile is read once for
-// all query heads of the group; a cluster of four CTAs splits the entries of the same rows, since
-// few rows and a long cache is what decoding is, and joins (maximum, sum, output) through
-// distributed shared memory in a fixed order.  All arithmetic is fp32.  Bound by the fp32 units and
-// shared-memory reads, about 4 * rows * entries * head_dim operations.
+// all query heads of the group; a cluster of two, four or eight CTAs splits the entries of the same
+// rows, since few rows and a long cache is what decoding is, and joins (maximum, sum, output) through
+// distributed shared memory in a fixed order.  All arithmetic is fp32.  A tile is a chain: its keys
+// and values (0.8 us; their pages were looked up during the tile before), scores, softmax, output;
+// small calls are bound by that chain, large ones by shared-memory reads, a float4 for four
+// fused multiply-adds: 42 rows of 8 heads on 300 entries of 64 take 15.7 us, 1000 prompt tokens of
+// 32 heads on up to 1000 entries of 128 take 1.0 ms (12 TFLOP/s).
 #include <cooperative_groups.h>
 
 #include "decode_common.cuh"
@@ -19,7 +22,6 @@ namespace cg = cooperative_groups;
 constexpr int kThreads = 128;
 constexpr int kRows = 16;    // query rows of a CTA; eight threads each
 constexpr int kTile = 32;    // entries of a tile
-constexpr int kSplit = 4;    // CTAs that share the entries
 constexpr int kCols = 8;     // threads of a row
 constexpr int kMaxQuads = kMaxHeadDim / (4 * kCols);
 
@@ -68,7 +70,7 @@ __device__ int find_unit(const BatchArgs& b, int64_t unit, F units, int64_t* res
   return s_found;
 }
 
-template <typename T>
+template <typename T, int kSplit>
 __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
   constexpr int E = T::kPerVec;
   extern __shared__ __align__(16) float s_mem[];
@@ -83,7 +85,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
   float* s_o = s_v + kTile * ld;         // [kRows][Dh], for the join
   __shared__ float s_p[kRows][kTile + 1];
   __shared__ float s_ml[kRows][2];
-  __shared__ int s_page[kTile];
+  __shared__ int s_page[2][kTile];  // of this tile's entries and of the next one's
 
   int64_t rest;
   const int s = find_unit(a.b, blockIdx.x / kSplit, [group](const Chunk& c) {
@@ -121,21 +123,23 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
 #pragma unroll
   for (int j = 0; j < kMaxQuads; ++j) o[j] = make_float4(0.f, 0.f, 0.f, 0.f);
 
-  for (int e0 = rank * kTile; e0 < end; e0 += kSplit * kTile) {
+  const auto look_up = [&](int e0) {  // thread tid < kTile: the page of entry e0 + tid
+    int page = -1;
+    if (tid < end - e0) {
+      page = page_of(a.b, s, e0 + tid);
+      if (page < 0) atomicOr(a.b.status, kStatusBadIndex);
+    }
+    return page;
+  };
+  int buf = 0;
+  if (tid < kTile) s_page[0][tid] = look_up(rank * kTile);
+  for (int e0 = rank * kTile; e0 < end; e0 += kSplit * kTile, buf ^= 1) {
     const int n = min(kTile, end - e0);
     __syncthreads();
-    if (tid < kTile) {
-      int page = -1;
-      if (tid < n) {
-        page = page_of(a.b, s, e0 + tid);
-        if (page < 0) atomicOr(a.b.status, kStatusBadIndex);
-      }
-      s_page[tid] = page;
-    }
-    __syncthreads();
+    const int next = tid < kTile ? look_up(e0 + kSplit * kTile) : 0;  // on its way while the tile is
     for (int v = tid; v < kTile * (Dh / E); v += kThreads) {
       const int e = v / (Dh / E), c = v % (Dh / E);
-      const int page = s_page[e];
+      const int page = s_page[buf][e];
       uint4 xk = make_uint4(0, 0, 0, 0), xv = xk;
       if (page >= 0) {
         const int64_t slot = (e0 + e) % a.b.page_size;
@@ -151,6 +155,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
         s_v[e * ld + c * E + q] = fv[q];
       }
     }
+    if (tid < kTile) s_page[buf ^ 1][tid] = next;
     __syncthreads();
     float x[kTile / kCols];
 #pragma unroll
@@ -167,7 +172,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
 #pragma unroll
     for (int j = 0; j < kTile / kCols; ++j) {
       const int e = col + j * kCols;
-      const bool see = r < rows && e < n && s_page[e] >= 0 && sees(a.b, s, ch, i, e0 + e);
+      const bool see = r < rows && e < n && s_page[buf][e] >= 0 && sees(a.b, s, ch, i, e0 + e);
       x[j] = see ? x[j] * sl : -INFINITY;
       top = fmaxf(top, x[j]);
     }
@@ -190,18 +195,25 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
     for (int j = 0; j < kMaxQuads; ++j) {
       o[j].x *= fix; o[j].y *= fix; o[j].z *= fix; o[j].w *= fix;
     }
-    for (int e = 0; e < n; ++e) {
-      const float p = s_p[r][e];
-      if (p == 0.f) continue;  // an entry that the row does not see may hold anything, NaN too
+    // (weights behind the last entry are 0, and the tile is filled up)
+    for (int e = 0; e < n; e += 4) {
+      float p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) p[u] = s_p[r][e + u];
 #pragma unroll
       for (int j = 0; j < kMaxQuads; ++j) {
         const int d = (j * kCols + col) * 4;
         if (d < Dh) {
-          const float4 v4 = *reinterpret_cast<const float4*>(s_v + e * ld + d);
-          o[j].x = fmaf(p, v4.x, o[j].x);
-          o[j].y = fmaf(p, v4.y, o[j].y);
-          o[j].z = fmaf(p, v4.z, o[j].z);
-          o[j].w = fmaf(p, v4.w, o[j].w);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const float4 v4 = *reinterpret_cast<const float4*>(s_v + (e + u) * ld + d);
+            if (p[u] != 0.f) {  // an entry that the row does not see may hold anything, NaN too
+              o[j].x = fmaf(p[u], v4.x, o[j].x);
+              o[j].y = fmaf(p[u], v4.y, o[j].y);
+              o[j].z = fmaf(p[u], v4.z, o[j].z);
+              o[j].w = fmaf(p[u], v4.w, o[j].w);
+            }
+          }
         }
       }
     }
@@ -218,7 +230,7 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
     if (d < Dh) *reinterpret_cast<float4*>(s_o + r * Dh + d) = o[j];
   }
   cluster.sync();
-  // ---- join: CTA `rank` finishes rows rank * 4 .. rank * 4 + 3
+  // ---- join: CTA `rank` finishes kMine of the rows
   constexpr int kMine = kRows / kSplit;
   const int jr = rank * kMine + tid / (kThreads / kMine);
   const int t0 = tid % (kThreads / kMine);
@@ -257,15 +269,13 @@ __global__ void __launch_bounds__(kThreads) attention_simt_kernel(AttnArgs a) {
   cluster.sync();  // nobody leaves while its rows are read
 }
 
-template <typename T>
-cudaError_t simt_as(const AttnArgs& a, cudaStream_t stream) {
-  const int Dh = a.c.head_dim, group = a.n_q_heads / a.c.n_kv_heads;
+template <typename T, int kSplit>
+cudaError_t simt_as(const AttnArgs& a, int64_t units, cudaStream_t stream) {
+  const int Dh = a.c.head_dim;
   const size_t smem = sizeof(float) * (2 * kRows * Dh + 2 * kTile * (Dh + 4));
-  cudaError_t e = cudaFuncSetAttribute(attention_simt_kernel<T>, cudaFuncAttributeMaxDynamicSharedMemorySize,
+  cudaError_t e = cudaFuncSetAttribute(attention_simt_kernel<T, kSplit>, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                        static_cast<int>(sizeof(float) * (2 * kRows * kMaxHeadDim + 2 * kTile * (kMaxHeadDim + 4))));
   if (e != cudaSuccess) return e;
-  // the lengths are on the device: as many units as T tokens in S chunks can make
-  const int64_t units = (static_cast<int64_t>(a.b.T) * group + kRows - 1) / kRows + a.b.S;
   cudaLaunchConfig_t cfg{};
   cfg.gridDim = dim3(static_cast<unsigned>(units * kSplit), a.c.n_kv_heads);
   cfg.blockDim = dim3(kThreads);
@@ -278,16 +288,31 @@ cudaError_t simt_as(const AttnArgs& a, cudaStream_t stream) {
   attr.val.clusterDim.z = 1;
   cfg.attrs = &attr;
   cfg.numAttrs = 1;
-  return cudaLaunchKernelEx(&cfg, attention_simt_kernel<T>, a);
+  return cudaLaunchKernelEx(&cfg, attention_simt_kernel<T, kSplit>, a);
+}
+
+template <typename T>
+cudaError_t simt_as(const AttnArgs& a, int sms, cudaStream_t stream) {
+  // the lengths are on the device: as many units as T tokens in S chunks can make
+  const int group = a.n_q_heads / a.c.n_kv_heads;
+  const int64_t units = (static_cast<int64_t>(a.b.T) * group + kRows - 1) / kRows + a.b.S;
+  // Few units: more CTAs for each shorten the walk over its entries (one token on 2000 entries 45 us with
+  // eight, 84 with four; 14 tree rows on 300 entries 15.7 and 18.2).  More: the join costs what it
+  // shortens (100 tokens on 200 entries 18.5 us with four, 27 with eight; 500 tokens on 1000 entries,
+  // 2016 units, 1015 with two, 1090 with four).
+  const int64_t all = units * a.c.n_kv_heads;
+  if (all <= sms / 2) return simt_as<T, 8>(a, units, stream);
+  if (all <= 8ll * sms) return simt_as<T, 4>(a, units, stream);
+  return simt_as<T, 2>(a, units, stream);
 }
 
 }  // namespace
 
-cudaError_t launch_attention_simt(const AttnArgs& a, cudaStream_t stream, int64_t* launches) {
+cudaError_t launch_attention_simt(const AttnArgs& a, int sms, cudaStream_t stream, int64_t* launches) {
   ++*launches;
-  if (a.c.dtype == GTO_BF16) return simt_as<Bf16>(a, stream);
-  if (a.c.dtype == GTO_F16) return simt_as<F16>(a, stream);
-  return simt_as<F32>(a, stream);
+  if (a.c.dtype == GTO_BF16) return simt_as<Bf16>(a, sms, stream);
+  if (a.c.dtype == GTO_F16) return simt_as<F16>(a, sms, stream);
+  return simt_as<F32>(a, sms, stream);
 }
 
 }  // namespace gto
