@@ -76,6 +76,7 @@ struct Tail {
   int64_t span, each, extra;    // this CTA's units; units of a CTA, CTAs that have one more
   int64_t off;                  // where the span begins: in block (seq, kvh, rb)
   int seq, kvh, rb;
+  Chunk chunk;                  // of that sequence
   uint32_t tmem;
   int abort;
 };
@@ -302,7 +303,7 @@ struct Walk {
       : b(batch), g(geo), heads(n_kv_heads), s(t.seq), kvh(t.kvh), rb(t.rb), nrb(0),
         off(static_cast<int>(t.off)), left(t.span) {
     if (left <= 0) return;
-    c = load_chunk(b, s);
+    c = t.chunk;
     nrb = g.blocks(c);
   }
   __device__ bool next(Item& it) {
@@ -372,8 +373,10 @@ __device__ __forceinline__ void plan(const BatchArgs& b, Geometry g, int heads, 
     return u;
   };
   int64_t mine = 0;
+  Chunk head{};  // of the run's first sequence
   for (int s = s0; s < s1; ++s) {
     const Chunk c = load_chunk(b, s);
+    if (s == s0) head = c;
     if (!c.ok && blockIdx.x == 0) atomicOr(b.status, kStatusBadIndex);
     mine += units_of(c) * heads;
   }
@@ -400,7 +403,7 @@ __device__ __forceinline__ void plan(const BatchArgs& b, Geometry g, int heads, 
   if (span > 0 && from >= begin && from < run) {
     int64_t off = from - begin;
     for (int s = s0; s < s1; ++s) {
-      const Chunk c = load_chunk(b, s);
+      const Chunk c = s == s0 ? head : load_chunk(b, s);
       const int64_t u = units_of(c);
       if (off >= u * heads) {
         off -= u * heads;
@@ -413,6 +416,7 @@ __device__ __forceinline__ void plan(const BatchArgs& b, Geometry g, int heads, 
       }
       for (int n = g.tiles(c, 0) + kOverhead; off >= n; n = g.tiles(c, ++rb) + kOverhead) off -= n;
       t.seq = s;
+      t.chunk = c;
       t.kvh = kvh;
       t.rb = rb;
       t.off = off;
@@ -1014,6 +1018,19 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
   const int n_rows = min(kJoinRows, meta.rows - first_row);
   const int64_t first = 2 * static_cast<int64_t>(blockIdx.x);
   auto slot = [first](int i) { return i == 0 ? first + 1 : first + 2 * i; };
+  // A thread has four columns of a row, eight rows of 128 columns at a time; its first parts are asked for
+  // before the weights are.
+  constexpr int kRowsAtOnce = kJoinThreads / (DH / 4), kFlight = 8;
+  constexpr int64_t kSlot = (DH / 4) * kBlock;
+  const int r8 = threadIdx.x % kRowsAtOnce, c = threadIdx.x / kRowsAtOnce;
+  const float4* part = p.part + static_cast<int64_t>(c) * kBlock + first_row;
+  float4 y[kFlight];
+  const auto fetch = [&](int r, int i0) {
+#pragma unroll
+    for (int q = 0; q < kFlight; ++q)
+      if (i0 + q < meta.parts) y[q] = part[slot(i0 + q) * kSlot + r];
+  };
+  if (r8 < n_rows) fetch(r8, 0);
   // ---- a row's maximum and sum over the parts: lane = row, the warps share the parts
   float m = -INFINITY, l = 0.f;
   for (int i = warp; i < meta.parts; i += kJoinThreads / 32) {
@@ -1042,20 +1059,14 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
         l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
   }
   __syncthreads();
-  // ---- outputs: eight rows at a time, a thread has four columns
-  constexpr int kRowsAtOnce = kJoinThreads / (DH / 4);
-  const int r8 = threadIdx.x % kRowsAtOnce, c = threadIdx.x / kRowsAtOnce;
+  // ---- outputs
   for (int r = r8; r < n_rows; r += kRowsAtOnce) {
     float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-    const float4* src = p.part + static_cast<int64_t>(c) * kBlock + first_row + r;
-    constexpr int64_t kSlot = (DH / 4) * kBlock;
-    for (int i = 0; i < meta.parts; i += 4) {
-      float4 y[4];
+    if (r != r8) fetch(r, 0);
+    for (int i = 0; i < meta.parts; i += kFlight) {
+      if (i > 0) fetch(r, i);
 #pragma unroll
-      for (int q = 0; q < 4; ++q)
-        if (i + q < meta.parts) y[q] = src[slot(i + q) * kSlot];
-#pragma unroll
-      for (int q = 0; q < 4; ++q)
+      for (int q = 0; q < kFlight; ++q)
         if (i + q < meta.parts) {
           const float w = s_w[i + q][r];
           o.x = fmaf(y[q].x, w, o.x);
@@ -1066,10 +1077,10 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     }
     const int row = meta.row0 + first_row + r;
     const int64_t at = (meta.tok0 + row / group) * a.n_q_heads + meta.kvh * group + row % group;
-    uint2 y;
-    y.x = pack2<T>(o.x, o.y);
-    y.y = pack2<T>(o.z, o.w);
-    reinterpret_cast<uint2*>(a.out + at * static_cast<int64_t>(DH * 2))[c] = y;
+    uint2 packed;
+    packed.x = pack2<T>(o.x, o.y);
+    packed.y = pack2<T>(o.z, o.w);
+    reinterpret_cast<uint2*>(a.out + at * static_cast<int64_t>(DH * 2))[c] = packed;
   }
 }
 
