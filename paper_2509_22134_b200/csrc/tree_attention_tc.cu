@@ -1,31 +1,45 @@
-// gto_tree_attention on the tensor cores: 16-bit tensors, heads of 64 or 128.
+// gto_tree_attention on the tensor cores: 16-bit tensors, heads of 64 or 128, pages of a multiple of 8.
 //
 // Rows.  A query row is one token and one of the query heads that share a key head; the rows of a
 // chunk and key head are cut into blocks of 256, two tiles of 128 (the M of the matrix
 // instruction), so that a tile of keys and values read once serves up to 256 rows.  With 128 rows
-// or fewer (single tokens, small trees) the two halves of the CTA take the even and the odd tiles
+// or fewer (single tokens, small trees) the two streams of the CTA take the even and the odd tiles
 // of the same rows instead and join at the end, which halves the dependent chain product -> softmax
 // -> product that a tile costs.
 //
-// Work.  A block of rows costs one unit for each 128 cache entries that it sees, plus kOverhead.
+// Work.  A block of rows costs one unit for each 64 cache entries that it sees, plus kOverhead.
 // All units of the call, in the order (sequence, key head, block, entries), are cut into as
 // many equal spans as there are SMs; every CTA takes one.  A block that a cut goes through leaves
 // its unnormalised parts in the workspace and a second, small kernel joins them in the order of
 // the entries.  The lengths are read on the device; the cut depends on nothing else, so that equal
 // calls give equal bits.
 //
-// A CTA is 12 warps: two groups of four own a tile's 128 rows, one thread a row, and do the
-// softmax and the epilogue; one warp issues the copies of keys and values (TMA boxes out of the
-// pages into a ring of stages), one the matrix instructions, two the copies of queries and the
-// tidying of tiles at the end of a sequence.  Scores, weights and accumulators live in tensor
-// memory: S (128 columns, for both groups in turn: a group takes its scores into registers at once),
-// the weights P0 P1 (64 each), the outputs O0 O1.
+// A CTA is 12 warps.  Eight do the softmax and the epilogue, four for each of two streams, one thread a
+// row.  One copies keys, one values and queries (TMA boxes out of the pages, into a ring of stages
+// each: keys are free for the next tile long before the values are).  Two issue the matrix
+// instructions, one a stream, so that one waits while the other issues.  Tensor memory holds for each
+// stream two buffers of scores (64 columns; the weights take the first 32 of theirs) and the output
+// (128): a stream's scores lie ready, two tiles ahead of its products with the values, when a softmax ends.
 //
 // Rounding.  Scores, maxima, sums and outputs are fp32; the weights are rounded to the 16-bit type
 // to be an operand of the second product (half a step each, independent errors), while their sum
 // is taken before that rounding.  The reference maximum of a row follows its true maximum only when
 // it has risen by more than 8 in log2 units: weights stay below 2^8, and most tiles need no
 // rescaling of the output.
+//
+// What bounds it (32 query heads, 8 key heads of 128; B200 at 1.7 to 1.97 GHz).  Single tokens: the copies;
+// 128 sequences of 1500 to 6000 entries take 341 us, 5.8 TB/s.  Trees and prompts: a step of 64
+// entries on 256 rows takes 2240 to 2460 cycles, where the matrix instructions need 1280 (a score
+// product of N = 64 reads 6 KB of operands from shared memory in 48 cycles, which is all that it
+// gives, in place of the 32 that the product would need) and the exponentials 1024: a stream's own
+// chain (scores to registers and their maximum 500, exponentials 1180 where two warps of a scheduler
+// have them at once, waits and hand-overs 700) is longer than either.  32 trees of 61 tokens on 1000 to 4000
+// entries take 134 us, four prompts of up to 2048 tokens on up to 6000 cached ones 379 us
+// (805 TFLOP/s of the products that are not masked).  One token of one sequence on 8000 entries takes
+// 20.7 us: 3 until the span is known, 10 for the tiles, 6 for the join.
+// Measured and slower: scores of 128 entries in one product (144 and 415 us: no second buffer), 16 warps for
+// the softmax (152, 424), next scores into registers during the exponentials (149), a part of the
+// exponentials as a polynomial (no gain), one warp for all matrix instructions (158).
 #include <cuda.h>
 
 #include "decode_common.cuh"
