@@ -387,7 +387,7 @@ gto_status gto_decode_destroy(gto_decode_ctx* ctx);
 /* Keys and values of the batch into the cache, queries rotated on the way.  q, k, v: rows of
  * n_heads * head_dim contiguous elements, row t at t * stride (elements, a multiple of 16
  * bytes: they may be slices of one projection); q_out: dense [T, n_q_heads, head_dim], may be
- * q itself where q is dense; q and q_out may both be NULL.  Token i of the lead has position
+ * q itself where q is dense, and overlaps neither k nor v; q and q_out may both be NULL.  Token i of the lead has position
  * base + i, node a of the tree base + lead - 1 + node_depth[a].
  * q_norm / k_norm ([head_dim], kv_dtype, or NULL): the head is first scaled to unit mean
  * square and multiplied by the weights.  Then the pair (x_i, x_{i + rope_dims/2}) is rotated by

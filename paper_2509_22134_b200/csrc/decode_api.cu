@@ -209,6 +209,9 @@ gto_status gto_kv_append(gto_decode_ctx* ctx, const gto_batch* batch, const gto_
     const bool in_place = q == q_out && q_stride * e == q_row;
     if (!in_place && overlap(q, span(a.b.T, q_stride * e, q_row), q_out, static_cast<size_t>(a.b.T) * q_row))
       return GTO_ERR_INVALID_ARG;
+    if (overlap(k, span(a.b.T, k_stride * e, kv_row), q_out, static_cast<size_t>(a.b.T) * q_row) ||
+        overlap(v, span(a.b.T, v_stride * e, kv_row), q_out, static_cast<size_t>(a.b.T) * q_row))
+      return GTO_ERR_INVALID_ARG;
   }
   if (c.rope_dims > 0 && !table(inv_freq, 8)) return GTO_ERR_INVALID_ARG;
   if ((q_norm && !aligned(q_norm, 16)) || (k_norm && !aligned(k_norm, 16))) return GTO_ERR_INVALID_ARG;

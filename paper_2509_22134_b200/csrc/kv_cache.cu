@@ -3,7 +3,7 @@
 // bounds them: append reads and writes (n_q + 2 n_kv) * head_dim values a token once, commit reads
 // and writes 2 * n_kv * head_dim values an accepted token and layer once.
 //
-// Measured, heads of 128: eight prompts of 900 to 4000 tokens, 32 query and 32 key heads, 186 us (96 % of the
+// Measured, heads of 128: eight prompts of up to 4000 tokens, 40 query and 40 key heads, 186 us (96 % of the
 // copy rate); 64 trees of 61 tokens, 32 and 8 heads, 24.7 us, of which 14.9 are the bytes and the rest
 // the chain place -> position -> rotation of three waves of CTAs.  Asking for the rows before that
 // chain cost more in registers than it hid (26 to 32 us), prefetching them into L2 too (26 us);

@@ -99,9 +99,9 @@ def draft_trees(tree: dict, b0: int = 0, b1: int | None = None, t: int = 0) -> d
 class DecodeStep:
     """Decoding with draft trees: S sequences over a paged cache of n_layers layers.
 
-    A step is begin(), attend() for every layer, verify() and commit(); nothing waits for the device, and a
-    step can be captured into a CUDA graph.  kv_len holds the cached entries of every sequence; page_table
-    is the caller's to fill (a page may be added between steps).
+    A step is begin(), attend() for every layer, verify() and commit(), all on the current stream; nothing
+    waits for the device, and a step can be captured into a CUDA graph.  kv_len holds the cached entries of
+    every sequence; page_table is the caller's to fill (a page may be added between steps).
     """
 
     def __init__(self, cfg: gto.gto_decode_config, n_layers: int, inv_freq, device="cuda:0"):
@@ -132,20 +132,20 @@ class DecodeStep:
         if trees is not None:
             self.batch.update({n: trees[n] for n in ("node_mask", "node_depth", "n_nodes") if n in trees})
 
-    def attend(self, layer: int, q, k, v, out, lse=None, q_norm=None, k_norm=None, stream=None):
+    def attend(self, layer: int, q, k, v, out, lse=None, q_norm=None, k_norm=None):
         """Keys and values of one layer into its cache, then the attention of the step's tokens over it."""
         rotated = self.q_rotated[:q.shape[0]]
         gto.gto_kv_append(self.ctx, self.batch, q, k, v, rotated, self.k_cache[layer], self.v_cache[layer],
-                          self.inv_freq, q_norm, k_norm, stream)
-        gto.gto_tree_attention(self.ctx, self.batch, rotated, self.k_cache[layer], self.v_cache[layer], out, lse, stream)
+                          self.inv_freq, q_norm, k_norm)
+        gto.gto_tree_attention(self.ctx, self.batch, rotated, self.k_cache[layer], self.v_cache[layer], out, lse)
 
-    def verify(self, trees: dict, target, d2t, temperature, u_node, u_bonus, stream=None) -> dict:
-        gto.gto_verify_tree(self.ctx, trees, target, d2t, temperature, u_node, u_bonus, self.verdict, stream)
+    def verify(self, trees: dict, target, d2t, temperature, u_node, u_bonus) -> dict:
+        gto.gto_verify_tree(self.ctx, trees, target, d2t, temperature, u_node, u_bonus, self.verdict)
         return self.verdict
 
-    def commit(self, stream=None):
+    def commit(self):
         """Keeps the accepted nodes' entries in all layers; kv_len then counts them."""
-        gto.gto_kv_commit(self.ctx, self.batch, self.verdict, self.k_cache, self.v_cache, self.kv_len, stream)
+        gto.gto_kv_commit(self.ctx, self.batch, self.verdict, self.k_cache, self.v_cache, self.kv_len)
 
     def status(self) -> int:
         return gto.gto_decode_status(self.ctx)

@@ -446,3 +446,68 @@ def test_calls_without_sequences_or_tokens_do_nothing(dtype):
     assert torch.all(out == 5.0)
     bits = torch.int16 if dtype == "bf16" else torch.int32
     assert torch.equal(k.view(bits), c.dk.view(bits)) and torch.equal(v.view(bits), c.dv.view(bits))
+
+
+# ------------------------------------------------------------------ where the kernels choose other variants
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype,V", [("f32", 393216), ("bf16", 786432), ("f16", 700000)])
+@pytest.mark.parametrize("S", [2, 41])
+def test_verify_the_longest_rows(dtype, V, S):
+    """Rows of up to 1.5 MB, few trees and many."""
+    from paper_2509_22134_b200 import binding as gto
+    from test_decode_gpu import check_verdict, run_verify, verify_case
+    if S > 2:
+        V = V // 128 * 8          # (16-byte rows)
+    c = verify_case(np.random.default_rng(V + S), S, 5, 3, V, V, dtype)
+    ctx, out = run_verify(gto, c, 3, V, V, dtype)
+    assert gto.gto_decode_status(ctx) == 0
+    for s in range(S):
+        check_verdict(c, s, out, 3)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("q_lens,kv_lens,shape,page,g", [
+    ([700], [900], (32, 8, 64), 16, 0), ([40, 61, 200, 61], [45, 300, 201, 77], (32, 16, 256), 5, 40),   # two CTAs a unit
+    ([61, 61], [400, 90], (16, 2, 128), 9, 60), ([1], [1000], (2, 1, 256), 3, 0)])                        # four, eight
+def test_fp32_attention_with_other_numbers_of_ctas(q_lens, kv_lens, shape, page, g):
+    from paper_2509_22134_b200 import binding as gto
+    c = dc.Case(q_lens, kv_lens, *shape, page, "f32", g, 6, seed=len(q_lens))
+    scale = c.dh ** -0.5
+    ctx = c.ctx(gto, softmax_scale=scale)
+    out = torch.full((c.T, c.hq, c.dh), 5.0, device=DEV)
+    z = torch.full((c.T, c.hq), 5.0, device=DEV)
+    gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=z)
+    assert gto.gto_decode_status(ctx) == 0
+    bare = SimpleNamespace(**{**vars(c), "k": np.where(c.used[..., None, None], c.k, 0.0), "v": np.where(c.used[..., None, None], c.v, 0.0)})
+    compare_attention(c, scale, out, z, dc.Case.attention_on_device(bare, scale))
+
+
+@pytest.mark.gpu
+def test_append_refuses_rotated_queries_over_keys_or_values():
+    from paper_2509_22134_b200 import binding as gto
+    c = dc.Case([3], [10], 2, 2, 64, 16, "bf16", seed=1, poison=0.0)
+    ctx = c.ctx(gto)
+    f = torch.ones(32, dtype=torch.float64, device=DEV)
+    k, v = torch.zeros_like(c.dq), torch.zeros_like(c.dq)
+    for over in (k, v):
+        with pytest.raises(gto.GtoError) as e:
+            gto.gto_kv_append(ctx, c.batch, c.dq, k, v, over, c.dk, c.dv, f)
+        assert e.value.code == 1
+    assert gto.gto_decode_launch_count(ctx) == 0
+
+
+@pytest.mark.gpu
+def test_a_page_shared_by_two_sequences_is_read_by_both():
+    """A common prompt's pages in two rows of the table; each sequence's own entries behind it."""
+    from paper_2509_22134_b200 import binding as gto
+    for dtype in ("bf16", "f32"):
+        c = dc.Case([2, 2], [70, 70], 8, 2, 64, 16, dtype, seed=6, poison=None)
+        c.host["page_table"][1, :4] = c.host["page_table"][0, :4]
+        c.batch["page_table"].copy_(torch.from_numpy(c.host["page_table"]))
+        ctx = c.ctx(gto, softmax_scale=0.125)
+        out = torch.full((c.T, c.hq, c.dh), 5.0, dtype=c.dq.dtype, device=DEV)
+        z = torch.full((c.T, c.hq), 5.0, device=DEV)
+        gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=z)
+        assert gto.gto_decode_status(ctx) == 0
+        compare_attention(c, 0.125, out, z)
