@@ -2,8 +2,8 @@
 //
 // One thread-block cluster of eight CTAs per sequence.  At every context it visits, the CTAs go
 // through their shares of the target row once (seven warps, each with a range of its own, so that a
-// last token is looked for in one warp's range only), exchange (reference, sum) through distributed
-// shared memory, and an eighth warp of every CTA makes the same decisions about the children from
+// last token is looked for in one warp's range only), tell one another (reference, sum) by stores into
+// each other's shared memory that a barrier there counts, and an eighth warp of every CTA makes the same decisions about the children from
 // the same numbers.  Where the walk ends, the CTA whose range the random number falls into reads that
 // range again and finds the token.  A row that is not visited is not read.
 //
@@ -16,22 +16,20 @@
 //
 // What bounds it is the chain: a sequence's rows come one after another, 8 of them for the longest
 // walk of the 128, and a row is a load's latency (0.8 us), a thread's 72 to 144 weights (1.5 to 4 us,
-// depending on how many CTAs share the SM), the exchange (1.2 us) and the decision (1 us); a draw from
+// depending on how many CTAs share the SM), the exchange and the decision (2.5 us); a draw from
 // the flat tail then costs the row in fp64 (4 us alone, 15 us when all sequences do).  Measured: one
-// tree of 32 000 ids 13.2 us, 128 trees of 128 256 ids 84 us (103 us with the row kept in shared
-// memory, which left room for three quarters of the clusters and took a second pass for the weights).
-#include <cooperative_groups.h>
-
+// tree of 32 000 ids 12.6 us, 128 trees of 128 256 ids 80 us (13.2 and 84 us with the cluster's own
+// barrier for the exchange; 103 us with the row kept in shared memory, which left room for three
+// quarters of the clusters and took a second pass for the weights).
 #include "decode_common.cuh"
 
 namespace gto {
 namespace {
 
-namespace cg = cooperative_groups;
-
 constexpr int kCluster = 8;                  // CTAs of a sequence
 constexpr int kWarps = 7;                    // that share the row
 constexpr int kWidth = 8;                    // lanes that their sums take
+constexpr int kLost = -4;                    // another CTA was not heard of
 constexpr int kThreads = (kWarps + 1) * 32;  // and one that knows the tree and decides
 
 // A thread's vectors of a row come through shared memory, kBatch at a time, kGroups batches on their way.
@@ -50,10 +48,9 @@ constexpr float kReach = 4.f;
 // added in fp32, in five levels (5 * 2^-24), the rest in fp64.  In all below 3.5e-6.
 constexpr double kSlack = 4e-6;
 
-struct Part {
-  double sum;     // of the CTA's weights, relative to the CTA's own maximum
+struct alignas(16) Part {
+  double sum;     // of the CTA's weights, relative to the CTA's own reference; NaN: it saw one
   uint64_t best;  // key of the CTA's largest logit (with its id for the greedy walk)
-  int bad;        // saw NaN
 };
 
 __device__ __forceinline__ double sum64(double v) {
@@ -150,10 +147,36 @@ __device__ __forceinline__ float weights(const uint4& v, float m, float c2) {
   return a + b;
 }
 
-// A 4- or 8-byte value into the same place of another CTA's shared memory.
-template <typename V>
-__device__ __forceinline__ void push(cg::cluster_group& cluster, V* place, int to, V value) {
-  *cluster.map_shared_rank(place, to) = value;
+// ---- what a CTA tells the others: a store into their shared memory that their barrier counts
+__device__ __forceinline__ uint32_t smem_of(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
+__device__ __forceinline__ uint32_t in_cta(uint32_t addr, int cta) {
+  uint32_t r;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
+  return r;
+}
+__device__ __forceinline__ void tell(uint32_t to, uint64_t a, uint64_t b, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(to), "l"(a),
+               "l"(b), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void tell(uint32_t to, uint32_t a, uint32_t bar) {
+  asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.b32 [%0], %1, [%2];" ::"r"(to), "r"(a), "r"(bar)
+               : "memory");
+}
+__device__ __forceinline__ void expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+// Waits for the phase of that parity, at most about two seconds; false if it has not ended.
+__device__ __forceinline__ bool heard(uint32_t bar, uint32_t parity) {
+  uint32_t ok = 0;
+  for (int i = 0; i < 20000 && !ok; ++i)
+    asm volatile(
+        "{\n .reg .pred p;\n mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2, 100000;\n"
+        " selp.u32 %0, 1, 0, p;\n}"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity)
+        : "memory");
+  return __all_sync(kFull, ok);
 }
 
 template <typename T, int kResident>
@@ -163,6 +186,7 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
   extern __shared__ __align__(16) unsigned char s_raw[];  // vectors on their way; a warp's range, where the last token is
   __shared__ Part s_part[2][kCluster];  // what the CTAs say of a row, sent by each to all
   __shared__ int s_redo;                // sent by the owner of the last token
+  __shared__ uint64_t s_bar[3];         // that s_part[0], s_part[1], s_redo have come
   __shared__ double s_wsum[kWarps];
   __shared__ float s_wmax[kWarps];
   __shared__ int s_wbad[kWarps], s_wid[kWarps];
@@ -174,11 +198,16 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
   __shared__ int s_from, s_out;
   __shared__ float s_top;
 
-  cg::cluster_group cluster = cg::this_cluster();
+  const uint32_t bar = smem_of(s_bar);
+  if (threadIdx.x == 0) {
+    for (int i = 0; i < 3; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(bar + i * 8) : "memory");
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+  }
+  __syncwarp();
   // the others' shared memory may be written once all have begun: waited for before the first push
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
   bool joined = false;
-  const int rank = static_cast<int>(cluster.block_rank());
+  const int rank = static_cast<int>(blockIdx.x % kCluster);
   const int s = blockIdx.x / kCluster;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool control = warp == kWarps;
@@ -252,6 +281,8 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
 
   int cur = -1, row = 0, len = 0, bonus = -1;
   bool exact = false;  // the row is summed again, in fp64
+  uint32_t asked = 0;  // answers of an owner so far
+  bool lost = false;   // another CTA was not heard of in time
   for (int step = 0; cold_ok; ++step) {
     const bool ex = exact || !(c2 < 1e30f);  // (a temperature next to 0 is beyond fp32)
     const char* z = a.target + (static_cast<int64_t>(s) * a.rows + row) * a.V_target * T::kBytes;
@@ -370,30 +401,28 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
       at = __reduce_min_sync(kFull, at);
       wrong = __any_sync(kFull, wrong);
       const double sum = sum_first<kWidth>(warp_sum);
-      if (lane < kCluster) {  // one thread for each CTA that hears it
-        Part* mine = &s_part[step & 1][rank];
-        push(cluster, &mine->sum, lane, sum);
-        push(cluster, &mine->best, lane, make_key(m_cta, at == 0x7fffffff ? 0 : at));
-        push(cluster, &mine->bad, lane, wrong);
-      }
+      const uint32_t here = bar + (step & 1) * 8;
+      if (lane == 0) expect(here, kCluster * sizeof(Part));
+      if (lane < kCluster)  // one thread for each CTA that hears it
+        tell(in_cta(smem_of(&s_part[step & 1][rank]), lane), __double_as_longlong(wrong ? NAN : sum),
+             make_key(m_cta, at == 0x7fffffff ? 0 : at), in_cta(here, lane));
     }
-    cluster.sync();
     // ---- the control warp of every CTA: the row's maximum and sum, and the children
     double scale = 0.0, total = 0.0, aim = 0.0, before_cta = 0.0;
     float M = 0.f;
     int removed = 0;
     if (control) {
+      // (a CTA is at most one step ahead of another: it needs the other's part of every step)
+      const bool all = heard(bar + (step & 1) * 8, step >> 1 & 1);
       uint64_t b = 0;
-      int wrong = 0;
       double part = 0.0;
       if (lane < kCluster) {
         const Part& p = s_part[step & 1][lane];
         b = p.best;
-        wrong = p.bad;
         part = p.sum;
       }
       const uint64_t row_best = warp_max_u64(b);
-      wrong = __any_sync(kFull, wrong);
+      const bool wrong = __any_sync(kFull, part != part);
       M = key_value(row_best);
       const bool sound = !wrong && M != -INFINITY && M != INFINITY;
       // a CTA's weights, to the row's maximum
@@ -469,15 +498,16 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
       }
       scale = __shfl_sync(kFull, scale, rank);
       if (lane == 0) {
-        s_child = sound ? child : -2;
+        s_child = !all ? kLost : sound ? child : -2;
         s_owner = greedy && sound ? key_id(row_best) : owner;
         s_close = close;
       }
     }
     __syncthreads();
     const int child = s_child;
-    if (child == -2) {
-      if (tid == 0) atomicOr(a.status, kStatusNonFinite);
+    if (child <= -2) {
+      lost = child == kLost;
+      if (tid == 0 && !lost) atomicOr(a.status, kStatusNonFinite);
       break;
     }
     if (s_close) {  // the same everywhere
@@ -508,7 +538,7 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
       } else {
         row = 1 + child;
       }
-      continue;  // the shared decision is rewritten only after the next cluster.sync()
+      continue;  // the shared decision is rewritten only after the next row
     }
     // ---- nothing accepted: the last token
     if (greedy) {
@@ -617,20 +647,36 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
           at += __shfl_sync(kFull, sum, 31);
         }
         if (found < 0) close = !ex;
-        if (lane < kCluster) push(cluster, &s_redo, lane, static_cast<int>(close));
+        if (!ex && lane < kCluster) tell(in_cta(smem_of(&s_redo), lane), close ? 1u : 0u, in_cta(bar + 16, lane));
         if (lane == 0 && !close) a.token[static_cast<int64_t>(s) * (a.D + 1) + len] = found >= 0 ? found : last;
       }
     }
-    cluster.sync();  // the owner's answer
-    if (!ex && s_redo) {
-      exact = true;
-      continue;
+    if (!ex) {  // the owner's answer
+      if (control) {
+        if (lane == 0) expect(bar + 16, sizeof(s_redo));
+        if (!heard(bar + 16, asked & 1) && lane == 0) s_redo = kLost;
+      }
+      ++asked;
+      __syncthreads();
+      if (s_redo == kLost) {
+        lost = true;
+        break;
+      }
+      if (s_redo) {
+        exact = true;
+        continue;
+      }
     }
     bonus = -3;  // written by the owner
     break;
   }
   if (!joined) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
-  // what the walk did not fill (nothing is sent to a CTA after the last cluster.sync() that it was in)
+  if (lost) {  // what is late may still come: nobody leaves before the others
+    if (tid == 0) atomicOr(a.status, kStatusTimeout);
+    asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+    asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  // What the walk did not fill.  (Else a CTA may leave: whatever the others sent it, it has waited for.)
   if (rank == 0) {
     if (tid == 0) {
       if (!cold_ok) atomicOr(a.status, kStatusNonFinite);
@@ -663,7 +709,7 @@ template <typename T>
 cudaError_t verify_as(const VerifyArgs& a, int sms, cudaStream_t stream) {
   // Two CTAs an SM may have 128 registers a thread: one tree of 32 000 ids took 13.2 us against 14.1 with
   // 64.  Where the sequences do not fit the device so, four: 128 trees of 128 256 ids took 84 us against
-  // 97 at three an SM (and 91 in clusters of four CTAs, four an SM).
+  // 97 at three an SM, and 91 in clusters of four CTAs (all with the cluster's barrier for the exchange).
   const bool few = static_cast<int64_t>(a.S) * kCluster <= 2ll * sms;
   return few ? verify_as<T, 2>(a, stream) : verify_as<T, 4>(a, stream);
 }
