@@ -77,7 +77,7 @@ __device__ __forceinline__ double scan64(double v, int lane) {
   return v;
 }
 
-// 2^x in fp64 for x <= 0, without branches, so that several run side by side (the library's exp took
+// 2^x in fp64 for x <= 4, without branches, so that several run side by side (the library's exp took
 // 300 cycles each, one after the other): Cody and Waite's reduction x = n + f, |f| <= 1/2, and the
 // polynomial of degree 10 with the least largest relative error there (by Remez's exchange:
 // 2.1e-16; 4.2e-16 in fp64).  Below 2^-1000 the result is 0; NaN gives NaN.
