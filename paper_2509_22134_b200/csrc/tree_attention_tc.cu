@@ -34,9 +34,9 @@
 // gives, in place of the 32 that the product would need) and the exponentials 1024: a stream's own
 // chain (scores to registers and their maximum 500, exponentials 1180 where two warps of a scheduler
 // have them at once, waits and hand-overs 700) is longer than either.  32 trees of 61 tokens on 1000 to 4000
-// entries take 134 us, four prompts of up to 2048 tokens on up to 6000 cached ones 379 us
-// (805 TFLOP/s of the products that are not masked).  One token of one sequence on 8000 entries takes
-// 20.7 us: 3 until the span is known, 10 for the tiles, 6 for the join.
+// entries take 131 us, four prompts of up to 2048 tokens on up to 6000 cached ones 376 us
+// (810 TFLOP/s of the products that are not masked).  One token of one sequence on 8000 entries takes
+// 20.0 us: 3 until the span is known, 10 for the tiles, 6 for the join.
 // Measured and slower: scores of 128 entries in one product (144 and 415 us: no second buffer), 16 warps for
 // the softmax (152, 424), next scores into registers during the exponentials (149), a part of the
 // exponentials as a polynomial (no gain), one warp for all matrix instructions (158).
@@ -51,7 +51,9 @@ constexpr int kThreads = 384;
 constexpr int kRows = 128;       // rows of a row tile (M of the matrix instruction)
 constexpr int kBlock = 2 * kRows;
 constexpr int kTile = 64;        // cache entries of a tile
-constexpr int kOverhead = 2;     // cost of a block beside its tiles, in tiles
+// Cost of a block beside its tiles (queries, first scores, epilogue), in tiles.  Measured with 2, 4, 6, 8, 12: one
+// token on 8000 entries 20.8, 20.2, 20.0, 19.9, 19.9 us, 32 trees 136, 134, 131, 131, 133, prompts 384, 382, 376, 379, 380.
+constexpr int kOverhead = 6;
 constexpr int kGoRing = 16;      // more than the value tiles that their ring can hold
 constexpr int kFewRows = 32;     // a block of no more rows is copied row by row
 constexpr float kLazy = 8.0f;    // log2 units the maximum may rise before the output is rescaled
