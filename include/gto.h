@@ -307,7 +307,8 @@ gto_status gto_kernel_times(gto_ctx* ctx, void* stream, double* total_ms, int64_
  * The functions take a gto_decode_ctx, which owns the workspace and a status word.  Calls
  * through one context share them: order them (one stream, events), and give every stream or
  * captured graph that may run at the same time a context of its own.  The calls can be
- * captured into a CUDA graph; lengths, tables and trees are read on the device at replay.
+ * captured into a CUDA graph, which the context has to outlive; lengths, tables and trees are
+ * read on the device at replay.
  * Every index is checked on the device before it is followed: a sequence with an inconsistent
  * q_start, kv_len, n_nodes or page_table entry is reported (GTO_ERR_BAD_INDEX) and skipped. */
 
