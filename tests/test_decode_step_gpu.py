@@ -511,3 +511,40 @@ def test_a_page_shared_by_two_sequences_is_read_by_both():
         gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=z)
         assert gto.gto_decode_status(ctx) == 0
         compare_attention(c, 0.125, out, z)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_sequences_than_a_cta_has_threads(dtype):
+    """1000 sequences, some without tokens, some with trees: the cut of the work goes through several of a thread's."""
+    from paper_2509_22134_b200 import binding as gto
+    rng = np.random.default_rng(12)
+    S, g = 1000, 5
+    nodes = rng.integers(0, g + 1, S)
+    lead = rng.choice([0, 1, 1, 1, 3], S)
+    nodes[lead == 0] = 0
+    q_lens = (lead + nodes).tolist()
+    kv_lens = [q + int(rng.integers(0, 200)) for q in q_lens]
+    c = dc.Case(q_lens, kv_lens, 4, 2, 64, 8, dtype, g, 3, nodes, seed=3, poison=None)
+    ctx = c.ctx(gto, softmax_scale=0.125)
+    out = torch.full((c.T, c.hq, c.dh), 5.0, dtype=c.dq.dtype, device=DEV)
+    z = torch.full((c.T, c.hq), 5.0, device=DEV)
+    gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=z)
+    assert gto.gto_decode_status(ctx) == 0
+    compare_attention(c, 0.125, out, z, c.attention_on_device(0.125))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("hq,hkv,dh", [(128, 1, 128), (100, 1, 64), (192, 2, 128), (256, 2, 64)])
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+def test_many_query_heads_on_a_key_head(dtype, hq, hkv, dh):
+    """A token's heads fill a row tile, or pass its end."""
+    from paper_2509_22134_b200 import binding as gto
+    c = dc.Case([1, 4, 9, 0, 2], [700, 4, 90, 3, 65], hq, hkv, dh, 16, dtype, 8, 3, [0, 3, 8, 0, 1], seed=hq, poison=None)
+    scale = dh ** -0.5
+    ctx = c.ctx(gto, softmax_scale=scale)
+    out = torch.full((c.T, hq, dh), 5.0, dtype=c.dq.dtype, device=DEV)
+    z = torch.full((c.T, hq), 5.0, device=DEV)
+    gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=z)
+    assert gto.gto_decode_status(ctx) == 0
+    compare_attention(c, scale, out, z, c.attention_on_device(scale))
