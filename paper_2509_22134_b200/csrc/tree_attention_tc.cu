@@ -22,10 +22,13 @@
 // (128): a stream's scores lie ready, two tiles ahead of its products with the values, when a softmax ends.
 //
 // Rounding.  Scores, maxima, sums and outputs are fp32; the weights are rounded to the 16-bit type
-// to be an operand of the second product (half a step each, independent errors), while their sum
-// is taken before that rounding.  The reference maximum of a row follows its true maximum only when
-// it has risen by more than 8 in log2 units: weights stay below 2^8, and most tiles need no
-// rescaling of the output.
+// to be an operand of the second product (half a step each), while their sum is taken before that
+// rounding.  A row's weights are 2^(score - reference).  The reference follows the row's maximum only
+// when that has risen by more than kLazy in log2 units, so that most tiles need no rescaling of the
+// output.  bf16 has fp32's exponents.  fp16 has normal numbers from 2^-14 to 2^16 only: its reference lies
+// kRaise below the maximum, weights go up to 2^(kRaise + kLazy) = 2^15, and those down to 2^-25 of the
+// row's largest keep the half step (a long flat tail behind one large score is made of such weights);
+// what is below 2^-36 of it is lost.
 //
 // What bounds it (32 query heads, 8 key heads of 128; B200 at 1.7 to 1.97 GHz).  Single tokens: the copies;
 // 128 sequences of 1500 to 6000 entries take 341 us, 5.8 TB/s.  Trees and prompts: a step of 64
@@ -56,7 +59,11 @@ constexpr int kTile = 64;        // cache entries of a tile
 constexpr int kOverhead = 6;
 constexpr int kGoRing = 16;      // more than the value tiles that their ring can hold
 constexpr int kFewRows = 32;     // a block of no more rows is copied row by row
-constexpr float kLazy = 8.0f;    // log2 units the maximum may rise before the output is rescaled
+// log2 units the maximum may rise before the output is rescaled, and by which the reference lies below it
+template <typename T>
+constexpr float kLazy = T::kNegInfElem == 0xff80u ? 8.0f : 4.0f;
+template <typename T>
+constexpr float kRaise = T::kNegInfElem == 0xff80u ? 0.0f : 11.0f;
 constexpr uint32_t kWaitTries = 20000;  // of a tenth of a millisecond
 
 template <int DH>
@@ -87,7 +94,7 @@ struct Tail {
   // only that it was issued (the product waits for the weights, which wait for `go`)
   uint64_t go[kGoRing];
   uint64_t scanned_both, scanned[2];
-  float ml[kRows][2];           // maximum and sum of the odd tiles' rows
+  float ml[kRows][2];           // reference and sum of the odd tiles' rows
   int64_t scan[kThreads / 32];
   int64_t span, each, extra;    // this CTA's units; units of a CTA, CTAs that have one more
   int64_t off;                  // where the span begins: in block (seq, kvh, rb)
@@ -753,7 +760,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int nt = it.t1 - it.t0;
       const int step = dual ? 1 : 2, j0 = dual ? 0 : st;
       const int first_masked = max(it.common / kTile, it.t0);  // tiles from here on are masked
-      float m = -INFINITY, l = 0.f;
+      float m = -INFINITY, l = 0.f;  // reference and sum
       if (it.alike && !__any_sync(kFull, valid)) {
         // a warp of rows that do not exist: their scores and weights may stay what they are
         for (int j = j0; j < nt && ok; j += step, ++seen) {
@@ -857,11 +864,11 @@ __global__ void __launch_bounds__(kThreads, 1)
             mask(tile);
             if (!ok) break;
           }
-          const float top = fmaxf(max_of(x[0]), max_of(x[1])) * sl;
+          const float top = fmaxf(max_of(x[0]), max_of(x[1])) * sl - kRaise<T>;  // the reference of these scores
           if (j == j0) {
             m = top;
           } else {
-            const bool rise = valid && top > m + kLazy;
+            const bool rise = valid && top > m + kLazy<T>;
             if (__any_sync(kFull, rise)) {
               // the product with the last weights is complete (those before it are: these scores were
               // issued after them)
@@ -1047,7 +1054,7 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
       if (i0 + q < meta.parts) y[q] = part[slot(i0 + q) * kSlot + r];
   };
   if (r8 < n_rows) fetch(r8, 0);
-  // ---- a row's maximum and sum over the parts: lane = row, the warps share the parts
+  // ---- a row's reference and sum over the parts: lane = row, the warps share the parts
   float m = -INFINITY, l = 0.f;
   for (int i = warp; i < meta.parts; i += kJoinThreads / 32) {
     const float2 ml = lane < n_rows ? p.part_ml[slot(i) * kBlock + first_row + lane] : make_float2(-INFINITY, 0.f);

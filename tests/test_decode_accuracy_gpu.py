@@ -1,0 +1,58 @@
+"""How exact the decoding step's attention is, on inputs where a coarser kernel would pass for a right one."""
+import numpy as np
+import pytest
+import torch
+
+import decode_cases as dc
+
+pytestmark = pytest.mark.gpu
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def gto():
+    from paper_2509_22134_b200 import binding
+    return binding
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("n,gap", [(60001, 17.6), (60001, 17.156), (300001, 17.6), (5000, 9.0)])
+def test_a_flat_tail_behind_one_large_score_is_kept(gto, n, gap, dh, dtype):
+    """One entry, of value 0, has a score `gap` above all others, which are equal: each of them weighs about 2^-25 of it
+    and together they are the whole output.  As many sequences as make every SM go through whole rows read one cache.
+
+    Tolerance.  The tail's weights are equal, so their roundings are too: half a step, relative to a weight as long as the
+    type holds it as a normal number (fp16: down to 2^-25 of the row's largest; 17.6 is 2^-25.4 of it, where a step is
+    2^0.4 times as large against the weight), and the output is rounded once: 2.4 half steps, 3 are allowed.  The score is a
+    product of two numbers and its scale is 1: both exact; exp in fp32: 2^-18 covers 2^-22 for a weight and 2^-24 |score| for
+    its argument.  Sums of equal terms err the same way at every step: a row's tiles of 64 go to two streams, `tiles`
+    each; the fp32 sum of the weights rounds once a tile, the output's accumulator four times and may cut (2^-23), both on a
+    sum that is half of the last one on the average."""
+    S, page = 160, 128
+    pages = -(-n // page)
+    k = torch.zeros((pages, page, 1, dh), dtype=torch.float64)
+    gen = torch.Generator().manual_seed(n + dh)
+    v = (1 + 0.25 * torch.randn(k.shape, generator=gen)).to(dc.TORCH[dtype])
+    k[0, 0, 0, 0] = gap / 8
+    v[0, 0] = 0
+    k = k.to(dc.TORCH[dtype])
+    top = float(k[0, 0, 0, 0]) * 8
+    w = np.exp(-top)
+    want = w * v.view(-1, dh)[:n].double().sum(0) / (1 + w * (n - 1))
+    q = torch.zeros((S, 1, dh), dtype=dc.TORCH[dtype], device=DEV)
+    q[:, :, 0] = 8
+    batch = dict(q_start=torch.arange(S + 1, dtype=torch.int32, device=DEV), kv_len=torch.full((S,), n, dtype=torch.int32, device=DEV),
+                 page_table=torch.arange(pages, dtype=torch.int32, device=DEV).repeat(S, 1))
+    cfg = gto.make_decode_config(S=S, T=S, n_q_heads=1, n_kv_heads=1, head_dim=dh, page_size=page, n_pages=pages, max_pages=pages,
+                                 dtype=dtype, softmax_scale=1.0)
+    ctx = gto.gto_decode_create(cfg, 0)
+    out, lse = torch.zeros_like(q), torch.zeros((S, 1), device=DEV)
+    gto.gto_tree_attention(ctx, batch, q, k.to(DEV), v.to(DEV), out, lse=lse)
+    assert gto.gto_decode_status(ctx) == 0
+    tiles = n / 128 + 1
+    err = (out.double().cpu()[:, 0] - want).abs()
+    assert torch.all(err <= want * (3 * dc.HALF_STEP[dtype] + 2.0 ** -18 + 4 * tiles * 2.0 ** -24)), float((err / want).max())
+    err = (lse.double().cpu() - (top + np.log1p(w * (n - 1)))).abs()
+    assert torch.all(err <= 2.0 ** -18 + tiles * 2.0 ** -25 + 2.0 ** -22 * top), float(err.max())
