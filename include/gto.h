@@ -309,8 +309,11 @@ gto_status gto_kernel_times(gto_ctx* ctx, void* stream, double* total_ms, int64_
  * captured graph that may run at the same time a context of its own.  The calls can be
  * captured into a CUDA graph, which the context has to outlive; lengths, tables and trees are
  * read on the device at replay.
- * Every index is checked on the device before it is followed: a sequence with an inconsistent
- * q_start, kv_len, n_nodes or page_table entry is reported (GTO_ERR_BAD_INDEX) and skipped. */
+ * Every index is checked on the device before it is followed.  A sequence whose q_start, kv_len or
+ * n_nodes contradict one another or the limits is reported (GTO_ERR_BAD_INDEX) and skipped; where
+ * q_start decreases, so are all sequences from there on.  A page_table entry that names no page is
+ * reported when it is needed: gto_kv_append leaves that token out, the rows of gto_tree_attention
+ * that look there are unspecified, gto_kv_commit skips the sequence. */
 
 typedef struct gto_decode_ctx gto_decode_ctx;
 

@@ -28,6 +28,10 @@ __device__ __forceinline__ Chunk load_chunk(const BatchArgs& b, int s) {
   return c;
 }
 
+// Whether q_start decreases over sequence s.  That sequence and all behind it are skipped: load_chunk looks at
+// one sequence alone, and only where q_start has not decreased are the tokens of two sequences apart.
+__device__ __forceinline__ bool falls(const BatchArgs& b, int s) { return b.q_start[s + 1] < b.q_start[s]; }
+
 // Page of cache entry t (t inside the sequence); -1 if the table names none.
 __device__ __forceinline__ int page_of(const BatchArgs& b, int s, int t) {
   const int p = b.page_table[static_cast<int64_t>(s) * b.max_pages + t / b.page_size];

@@ -26,7 +26,7 @@ __device__ __forceinline__ void turn(double position, double inv_freq, float& c,
   sincospif(2.0f * f, &s, &c);
 }
 
-// One CTA per token.  A group of `lanes` lanes (a power of two, at least half the 16-byte vectors
+// One CTA per token, and one that looks at all sequences for those that contradict themselves.  A group of `lanes` lanes (a power of two, at least half the 16-byte vectors
 // of a head) takes one head at a time; a lane holds the two vectors whose elements rotate into
 // one another.
 template <typename T, bool kInterleaved>
@@ -35,13 +35,29 @@ __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a,
   __shared__ float s_cos[kMaxHalf], s_sin[kMaxHalf];
   __shared__ int s_seq;
   const int tid = threadIdx.x, t = blockIdx.x;
+  if (t == a.b.T) {
+    for (int s = tid; s < a.b.S; s += kAppendThreads)
+      if (!load_chunk(a.b, s).ok) atomicOr(a.b.status, kStatusBadIndex);
+    return;
+  }
   if (tid == 0) s_seq = -1;
   __syncthreads();
-  for (int s = tid; s < a.b.S; s += kAppendThreads)
-    if (a.b.q_start[s] <= t && t < a.b.q_start[s + 1]) s_seq = s;
-  __syncthreads();
+  bool fall = false;
+  for (int s = tid; s < a.b.S; s += kAppendThreads) {
+    const int q0 = a.b.q_start[s], q1 = a.b.q_start[s + 1];
+    if (q0 <= t && t < q1) s_seq = s;
+    fall |= q1 < q0;
+  }
+  if (__syncthreads_or(fall)) {  // several sequences may have the token: the first counts, if q_start has not decreased before
+    if (tid == 0) {
+      s_seq = -1;
+      for (int s = 0; s < a.b.S && !falls(a.b, s); ++s)
+        if (a.b.q_start[s] <= t && t < a.b.q_start[s + 1]) s_seq = s;
+    }
+    __syncthreads();
+  }
   const int s = s_seq;
-  if (s < 0) return;  // a token of no sequence
+  if (s < 0) return;  // a token of no sequence, or of one that is skipped
   const Chunk ch = load_chunk(a.b, s);
   const int i = t - ch.q0;
   int page = -1, pos = 0;
@@ -171,6 +187,9 @@ constexpr int kCommitBatch = 8;
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(CommitArgs a) {
   const int s = blockIdx.x, layer = blockIdx.y, tid = threadIdx.x;
   const Chunk ch = load_chunk(a.b, s);
+  bool behind = false;  // a decrease of q_start, which the CTA of the sequence there reports
+  for (int j = tid; j < s; j += kCommitThreads) behind |= falls(a.b, j);
+  if (__syncthreads_or(behind)) return;
   if (ch.n == 0 && ch.ok) {
     if (layer == 0 && tid == 0) a.kv_len_out[s] = ch.len;
     return;
@@ -231,9 +250,9 @@ cudaError_t append_as(const AppendArgs& a, cudaStream_t stream) {
   int lanes = 1;
   while (lanes < a.c.head_dim / (2 * T::kPerVec)) lanes *= 2;
   if (a.interleaved)
-    kv_append_kernel<T, true><<<a.b.T, kAppendThreads, 0, stream>>>(a, lanes);
+    kv_append_kernel<T, true><<<a.b.T + 1, kAppendThreads, 0, stream>>>(a, lanes);
   else
-    kv_append_kernel<T, false><<<a.b.T, kAppendThreads, 0, stream>>>(a, lanes);
+    kv_append_kernel<T, false><<<a.b.T + 1, kAppendThreads, 0, stream>>>(a, lanes);
   return cudaGetLastError();
 }
 

@@ -26,11 +26,12 @@ constexpr int kCols = 8;     // threads of a row
 constexpr int kMaxQuads = kMaxHeadDim / (4 * kCols);
 
 // Sequence that work unit `unit` belongs to, where sequence s has units(chunk of s) of them; the
-// unit's number inside the sequence in *rest.  Called by the whole CTA; -1 past the last unit.
+// unit's number inside the sequence in *rest.  Called by the whole CTA; -1 past the last unit.  Sequences from
+// the first decrease of q_start on have none.
 template <typename F>
 __device__ int find_unit(const BatchArgs& b, int64_t unit, F units, int64_t* rest) {
   __shared__ int64_t s_scan[kThreads / 32];
-  __shared__ int s_found;
+  __shared__ int s_found, s_fall;
   __shared__ int64_t s_rest;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   if (tid == 0) s_found = -1;
@@ -38,20 +39,35 @@ __device__ int find_unit(const BatchArgs& b, int64_t unit, F units, int64_t* res
   for (int s0 = 0; s0 < b.S; s0 += kThreads) {
     const int s = s0 + tid;
     int64_t n = 0;
+    bool fall = false;
     if (s < b.S) {
       const Chunk c = load_chunk(b, s);
       if (c.ok) n = units(c);
       else atomicOr(b.status, kStatusBadIndex);
+      fall = !c.ok && falls(b, s);
     }
-    int64_t run = n;
+    int64_t run;
+    const auto scan = [&] {
+      run = n;
 #pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const int64_t y = __shfl_up_sync(kFull, run, o);
-      if (lane >= o) run += y;
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t y = __shfl_up_sync(kFull, run, o);
+        if (lane >= o) run += y;
+      }
+      __syncthreads();
+      if (lane == 31) s_scan[warp] = run;
+    };
+    scan();
+    const bool last = __syncthreads_or(fall);
+    if (last) {  // once more without the sequences that are skipped
+      if (tid == 0) s_fall = b.S;
+      __syncthreads();
+      if (fall) atomicMin(&s_fall, s);
+      __syncthreads();
+      if (s >= s_fall) n = 0;
+      scan();
+      __syncthreads();
     }
-    __syncthreads();
-    if (lane == 31) s_scan[warp] = run;
-    __syncthreads();
     int64_t total = 0;
     for (int w = 0; w < kThreads / 32; ++w) {
       if (w < warp) run += s_scan[w];
@@ -64,7 +80,7 @@ __device__ int find_unit(const BatchArgs& b, int64_t unit, F units, int64_t* res
     }
     before += total;
     __syncthreads();
-    if (s_found >= 0) break;
+    if (s_found >= 0 || last) break;
   }
   *rest = s_rest;
   return s_found;

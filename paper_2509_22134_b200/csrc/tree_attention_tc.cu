@@ -395,23 +395,35 @@ __device__ __forceinline__ void plan(const BatchArgs& b, Geometry g, int heads, 
     for (int i = 0; i < nrb; ++i) u += g.tiles(c, i) + kOverhead;
     return u;
   };
-  int64_t mine = 0;
+  int64_t mine, run;
   Chunk head{};  // of the run's first sequence
-  for (int s = s0; s < s1; ++s) {
-    const Chunk c = load_chunk(b, s);
-    if (s == s0) head = c;
-    if (!c.ok && blockIdx.x == 0) atomicOr(b.status, kStatusBadIndex);
-    mine += units_of(c) * heads;
-  }
-  int64_t run = mine;
+  for (int seqs = b.S;;) {  // once, or again without the sequences from the first decrease of q_start on
+    int fall = seqs;
+    mine = 0;
+    for (int s = s0; s < min(s1, seqs); ++s) {
+      const Chunk c = load_chunk(b, s);
+      if (s == s0) head = c;
+      if (!c.ok && blockIdx.x == 0) atomicOr(b.status, kStatusBadIndex);
+      if (!c.ok && falls(b, s)) fall = min(fall, s);
+      mine += units_of(c) * heads;
+    }
+    run = mine;
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int64_t y = __shfl_up_sync(kFull, run, o);
-    if (lane >= o) run += y;
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t y = __shfl_up_sync(kFull, run, o);
+      if (lane >= o) run += y;
+    }
+    if (lane == 31) t.scan[warp] = run;
+    if (tid == 0) {
+      t.span = 0;
+      t.seq = seqs;
+    }
+    if (!__syncthreads_or(fall < seqs)) break;
+    atomicMin(&t.seq, fall);
+    __syncthreads();
+    seqs = t.seq;
+    __syncthreads();  // (read by all before it is written again)
   }
-  if (lane == 31) t.scan[warp] = run;
-  if (tid == 0) t.span = 0;
-  __syncthreads();
   int64_t units = 0;
   for (int w = 0; w < kThreads / 32; ++w) {
     if (w < warp) run += t.scan[w];

@@ -1,0 +1,126 @@
+"""Batches whose tables contradict themselves: every call of a step skips the same sequences, and says so."""
+import numpy as np
+import pytest
+import torch
+
+import decode_cases as dc
+from oracle import decode_oracle as dec
+
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def gto():
+    from paper_2509_22134_b200 import binding
+    return binding
+
+
+FREQ = 10000.0 ** (-np.arange(32) / 32)
+
+
+def attend(gto, ctx, c, fill=5.0):
+    out = torch.full((c.T, c.hq, c.dh), fill, dtype=c.dq.dtype, device=DEV)
+    gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out)
+    return out.double().cpu().numpy()
+
+
+def put(gto, ctx, c):
+    x = c.tensor(c.rng.normal(size=(c.T, c.hq + 2 * c.hkv, c.dh)))
+    q_out = torch.full((c.T, c.hq, c.dh), 7.0, dtype=x.dtype, device=DEV)
+    k, v = c.dk.clone(), c.dv.clone()
+    gto.gto_kv_append(ctx, c.batch, x[:, :c.hq], x[:, c.hq:c.hq + c.hkv], x[:, c.hq + c.hkv:], q_out, k, v,
+                      torch.tensor(FREQ, device=DEV))
+    return x, q_out, k, v
+
+
+def set_starts(c, starts):
+    c.batch["q_start"].copy_(torch.tensor(starts, dtype=torch.int32))
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("starts,good", [
+    ([0, 5, 3, 3], (0,)),           # a chunk of -2 tokens
+    ([0, 5, 900, 901], (0,)),       # chunks that begin or end behind the tokens
+    ([0, 8, 4, 12], (0,)),          # two chunks with the same tokens, each possible by itself
+    ([3, 0, 4, 12], ()),            # nothing is certain from the first sequence on
+    ([0, 5, 5, -2147483648], (0, 1)),
+])
+def test_append_and_commit_report_sequences_that_contradict_themselves(gto, starts, good):
+    c = dc.Case([5, 3, 4], [30, 40, 50], 4, 2, 64, 16, "bf16", seed=1, poison=0.0)
+    set_starts(c, starts)
+    lens = np.diff(np.array(starts, np.int64))
+    c.host["q_start"] = np.concatenate([[0], np.cumsum([lens[s] if s in good else 0 for s in range(3)])]).astype(np.int32)
+    ctx = c.ctx(gto)
+    x, q_out, k, v = put(gto, ctx, c)
+    assert gto.gto_decode_status(ctx) == 8
+    y = x.double().cpu().numpy()
+    want_q, want_k, want_v = dec.append(c.host, y[:, :4], y[:, 4:6], y[:, 6:], c.k, c.v, 16, FREQ)
+    n = int(c.host["q_start"][-1])
+    assert np.array_equal(v.double().cpu().numpy(), want_v)
+    err = np.abs(k.double().cpu().numpy() - want_k)                   # (one rounding, as in test_append)
+    assert np.all(err <= np.abs(want_k).max() * 2.0 ** -20 + dc.HALF_STEP["bf16"] * np.abs(want_k))
+    err = np.abs(q_out.double().cpu().numpy()[:n] - want_q[:n])
+    assert np.all(err <= np.abs(want_q[:n]).max(initial=0) * 2.0 ** -20 + dc.HALF_STEP["bf16"] * np.abs(want_q[:n]))
+    assert torch.all(q_out[n:] == 7.0)
+    verdict = dict(accept_len=torch.zeros(3, dtype=torch.int32, device=DEV), path_node=torch.zeros((3, 1), dtype=torch.int32, device=DEV),
+                   token=torch.zeros((3, 2), dtype=torch.int32, device=DEV))
+    new_len = torch.full((3,), -5, dtype=torch.int32, device=DEV)
+    gto.gto_kv_commit(ctx, c.batch, verdict, k, v, new_len)
+    assert gto.gto_decode_status(ctx) == 8
+    assert new_len.tolist() == [[30, 40, 50][s] if s in good else -5 for s in range(3)]
+
+
+@pytest.mark.gpu
+def test_append_reports_a_sequence_without_tokens_whose_length_is_impossible(gto):
+    c = dc.Case([3, 0], [30, 40], 4, 2, 64, 16, "bf16", seed=1, poison=0.0)
+    ctx = c.ctx(gto)
+    put(gto, ctx, c)
+    assert gto.gto_decode_status(ctx) == 0
+    for bad in (-1, c.max_pages * 16 + 1):
+        c.batch["kv_len"][1] = bad
+        put(gto, ctx, c)
+        assert gto.gto_decode_status(ctx) == 8
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_skips_every_sequence_behind_a_decrease(gto, dtype):
+    c = dc.Case([8, 3, 4], [30, 40, 50], 4, 2, 64, 16, dtype, seed=2, poison=0.0)
+    ctx = c.ctx(gto)
+    whole = attend(gto, ctx, c)
+    assert gto.gto_decode_status(ctx) == 0
+    set_starts(c, [0, 8, 4, 12])
+    for _ in range(2):
+        got = attend(gto, ctx, c)
+        assert gto.gto_decode_status(ctx) == 8
+        # (the cut of the work is another one: parts are joined elsewhere, so that bits may differ by a rounding)
+        assert np.all(np.abs(got[:8] - whole[:8]) <= dc.HALF_STEP[dtype] * 4 * np.abs(whole[:8]).max())
+        assert np.all(got[8:] == 5.0)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("at", [0, 1, 127, 128, 383, 384, 700, 999])
+def test_a_decrease_among_a_thousand_sequences(gto, dtype, at):
+    rng = np.random.default_rng(at)
+    S = 1000
+    q_lens = rng.integers(1, 4, S).tolist()
+    c = dc.Case(q_lens, [q + int(rng.integers(0, 60)) for q in q_lens], 4, 2, 64, 8, dtype, seed=3, poison=0.0)
+    ctx = c.ctx(gto)
+    whole = attend(gto, ctx, c)
+    start = c.host["q_start"].copy()
+    start[at + 1:] -= start[at + 1] - start[at] + 1            # (sequence `at` has -1 tokens; what follows overlaps)
+    set_starts(c, start)
+    got = attend(gto, ctx, c)
+    assert gto.gto_decode_status(ctx) == 8
+    n = int(start[at])
+    assert np.all(np.abs(got[:n] - whole[:n]) <= dc.HALF_STEP[dtype] * 4 * np.abs(whole).max())
+    assert np.all(got[n:] == 5.0)
+    x, q_out, k, v = put(gto, ctx, c)
+    assert gto.gto_decode_status(ctx) == 8
+    assert torch.all(q_out[n:] == 7.0) and (n == 0 or not torch.any((q_out[:n] == 7.0).all(-1)))
+    verdict = dict(accept_len=torch.zeros(S, dtype=torch.int32, device=DEV), path_node=torch.zeros((S, 1), dtype=torch.int32, device=DEV),
+                   token=torch.zeros((S, 2), dtype=torch.int32, device=DEV))
+    new_len = torch.full((S,), -5, dtype=torch.int32, device=DEV)
+    gto.gto_kv_commit(ctx, c.batch, verdict, k, v, new_len)
+    assert new_len.tolist() == c.host["kv_len"][:at].tolist() + [-5] * (S - at)
