@@ -437,7 +437,8 @@ gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, cons
 /* Keeps the accepted nodes of every sequence: cache entry base + lead + path_node[s][j] is copied
  * to base + lead + j for j < accept_len[s], in all layers, and kv_len_out[s] = base + lead +
  * accept_len[s] (base + n for a sequence without a tree in this batch; untouched for one that is
- * skipped).  kv_len_out must not be batch->kv_len, which the whole call reads.  path_node must
+ * skipped).  batch is the step's, T among it: a sequence that gto_kv_append skipped for lying behind its T
+ * tokens is skipped here too.  kv_len_out must not be batch->kv_len, which the whole call reads.  path_node must
  * increase along the path, as gto_verify_tree writes it. */
 gto_status gto_kv_commit(gto_decode_ctx* ctx, const gto_batch* batch, const gto_verdict* verdict,
                          const gto_kv_cache* cache, int32_t* kv_len_out, void* stream);

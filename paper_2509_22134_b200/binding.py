@@ -433,9 +433,11 @@ def gto_verify_tree(ctx: DecodeCtx, tree: dict, target, d2t, temperature, u_node
         raise GtoError(code, "gto_verify_tree")
 
 
-def gto_kv_commit(ctx: DecodeCtx, batch: dict, verdict: dict, k_cache, v_cache, kv_len_out, stream=None):
-    """k_cache, v_cache: [n_pages, ...] of one layer or [n_layers, n_pages, ...] of all."""
-    code = _native.kv_commit(ctx.native, batch, verdict, k_cache, v_cache, kv_len_out, _stream_of(ctx, stream))
+def gto_kv_commit(ctx: DecodeCtx, batch: dict, verdict: dict, k_cache, v_cache, kv_len_out, stream=None, tokens=None):
+    """k_cache, v_cache: [n_pages, ...] of one layer or [n_layers, n_pages, ...] of all.  tokens: rows of the q, k and v that
+    the step's other calls were given, by which they judged the batch (default: the context's T, which skips nothing that
+    ends behind those rows)."""
+    code = _native.kv_commit(ctx.native, batch, verdict, k_cache, v_cache, kv_len_out, tokens, _stream_of(ctx, stream))
     if code:
         raise GtoError(code, "gto_kv_commit")
 

@@ -118,8 +118,8 @@ int64_t first_size(PyObject* o, const char* name) {
 }
 
 int32_t small(int64_t n, const char* name) {
-  if (n > INT32_MAX) {
-    PyErr_Format(PyExc_ValueError, "%s: too many rows", name);
+  if (n > INT32_MAX || n < 0) {
+    PyErr_Format(PyExc_ValueError, "%s: %lld rows", name, static_cast<long long>(n));
     throw Raised{};
   }
   return static_cast<int32_t>(n);
@@ -276,15 +276,20 @@ PyObject* verify_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
-// (ctx, batch, verdict, k_cache, v_cache, kv_len_out, stream)
+// (ctx, batch, verdict, k_cache, v_cache, kv_len_out, tokens, stream); tokens None: as many as the context takes
 PyObject* kv_commit(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  return guarded(n, 7, [&]() -> long {
+  return guarded(n, 8, [&]() -> long {
     const Ctx& c = context(a[0]);
-    const gto_batch b = batch_of(c, a[1], c.cfg.T);
+    int64_t T = c.cfg.T;
+    if (a[6] != Py_None) {
+      T = PyLong_AsLongLong(a[6]);
+      if (T == -1 && PyErr_Occurred()) throw Raised{};
+    }
+    const gto_batch b = batch_of(c, a[1], T);
     const gto_verdict v = verdict_of(c, a[2], b.S);
     const gto_kv_cache cache = cache_of(c, a[3], a[4], true);
     void* out = dense(c, a[5], "kv_len_out", at::kInt, I1{b.S});
-    return gto_kv_commit(c.handle, &b, &v, &cache, static_cast<int32_t*>(out), stream_of(a[6]));
+    return gto_kv_commit(c.handle, &b, &v, &cache, static_cast<int32_t*>(out), stream_of(a[7]));
   });
 }
 

@@ -119,6 +119,7 @@ class DecodeStep:
         self.verdict = gto.alloc_verdict(cfg, self.device)
         self.q_rotated = torch.empty((cfg.T, cfg.n_q_heads, cfg.head_dim), dtype=dtype, device=self.device)
         self.batch = None
+        self.tokens = None  # rows that this step's layers were given, the fewest
 
     def close(self):
         if self.ctx is not None:
@@ -129,12 +130,14 @@ class DecodeStep:
         """The tokens of this step: chunk s is q_start[s] .. q_start[s+1], what comes before the draft tree (a
         prompt, or the last step's token) and then the tree's nodes."""
         self.batch = {"q_start": q_start, "kv_len": self.kv_len + torch.diff(q_start), "page_table": self.page_table}
+        self.tokens = None
         if trees is not None:
             self.batch.update({n: trees[n] for n in ("node_mask", "node_depth", "n_nodes") if n in trees})
 
     def attend(self, layer: int, q, k, v, out, lse=None, q_norm=None, k_norm=None):
         """Keys and values of one layer into its cache, then the attention of the step's tokens over it."""
         rotated = self.q_rotated[:q.shape[0]]
+        self.tokens = q.shape[0] if self.tokens is None else min(self.tokens, q.shape[0])
         gto.gto_kv_append(self.ctx, self.batch, q, k, v, rotated, self.k_cache[layer], self.v_cache[layer],
                           self.inv_freq, q_norm, k_norm)
         gto.gto_tree_attention(self.ctx, self.batch, rotated, self.k_cache[layer], self.v_cache[layer], out, lse)
@@ -144,8 +147,9 @@ class DecodeStep:
         return self.verdict
 
     def commit(self):
-        """Keeps the accepted nodes' entries in all layers; kv_len then counts them."""
-        gto.gto_kv_commit(self.ctx, self.batch, self.verdict, self.k_cache, self.v_cache, self.kv_len)
+        """Keeps the accepted nodes' entries in all layers; kv_len then counts them.  A sequence that the other calls
+        skipped keeps its kv_len."""
+        gto.gto_kv_commit(self.ctx, self.batch, self.verdict, self.k_cache, self.v_cache, self.kv_len, tokens=self.tokens)
 
     def status(self) -> int:
         return gto.gto_decode_status(self.ctx)

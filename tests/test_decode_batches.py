@@ -124,3 +124,54 @@ def test_a_decrease_among_a_thousand_sequences(gto, dtype, at):
     new_len = torch.full((S,), -5, dtype=torch.int32, device=DEV)
     gto.gto_kv_commit(ctx, c.batch, verdict, k, v, new_len)
     assert new_len.tolist() == c.host["kv_len"][:at].tolist() + [-5] * (S - at)
+
+
+# ------------------------------------------------------------------ what a step did not write is not kept
+
+def small_step(gto, S=3, T=64, layers=2, g=0, max_pages=8):
+    from paper_2509_22134_b200.runner import DecodeStep
+    cfg = gto.make_decode_config(S=S, T=T, n_q_heads=4, n_kv_heads=2, head_dim=64, page_size=16, n_pages=S * max_pages,
+                                 max_pages=max_pages, dtype="bf16", g=g, D=3, V_draft=64, V_target=64)
+    step = DecodeStep(cfg, layers, FREQ, DEV)
+    step.page_table.copy_(torch.arange(S * max_pages, dtype=torch.int32).view(S, max_pages))
+    return step
+
+
+def layers_of(step, tokens, seed=0):
+    gen = torch.Generator(DEV).manual_seed(seed)
+    for i in range(step.k_cache.shape[0]):
+        x = torch.randn((tokens, 8, 64), generator=gen, device=DEV).to(torch.bfloat16)
+        out = torch.zeros((tokens, 4, 64), dtype=torch.bfloat16, device=DEV)
+        step.attend(i, x[:, :4], x[:, 4:6], x[:, 6:], out)
+
+
+@pytest.mark.gpu
+def test_a_chunk_behind_the_steps_tokens_is_not_committed(gto):
+    """Sequence 2's chunk ends behind the rows that the layers were given, but within what the context takes."""
+    step = small_step(gto)
+    step.begin(torch.tensor([0, 5, 9, 20], dtype=torch.int32, device=DEV))
+    layers_of(step, 12)
+    step.commit()
+    assert step.status() == 8
+    assert step.kv_len.tolist() == [5, 4, 0]
+    step.begin(torch.tensor([0, 1, 2, 13], dtype=torch.int32, device=DEV))   # and again, with all rows
+    layers_of(step, 13)
+    step.commit()
+    assert step.status() == 0
+    assert step.kv_len.tolist() == [6, 5, 11]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("tokens,want", [(None, [13]), (13, [13]), (12, [-5]), (0, [-5])])
+def test_commit_judges_a_batch_by_the_tokens_it_is_told(gto, tokens, want):
+    c = dc.Case([13], [13], 4, 2, 64, 16, "bf16", seed=1, poison=0.0)
+    verdict = dict(accept_len=torch.zeros(1, dtype=torch.int32, device=DEV), path_node=torch.zeros((1, 1), dtype=torch.int32, device=DEV),
+                   token=torch.zeros((1, 2), dtype=torch.int32, device=DEV))
+    new_len = torch.full((1,), -5, dtype=torch.int32, device=DEV)
+    ctx = c.ctx(gto)
+    gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, new_len, tokens=tokens)
+    assert gto.gto_decode_status(ctx) == (0 if want == [13] else 8)
+    assert new_len.tolist() == want
+    for bad, error in ((-1, ValueError), (1 << 40, ValueError), (c.T + 1, gto.GtoError), ("x", TypeError)):
+        with pytest.raises(error):
+            gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, new_len, tokens=bad)
