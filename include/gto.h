@@ -313,7 +313,7 @@ gto_status gto_kernel_times(gto_ctx* ctx, void* stream, double* total_ms, int64_
  * n_nodes contradict one another or the limits is reported (GTO_ERR_BAD_INDEX) and skipped; where
  * q_start decreases, so are all sequences from there on.  A page_table entry that names no page is
  * reported when it is needed: gto_kv_append leaves that token out, the rows of gto_tree_attention
- * that look there are unspecified, gto_kv_commit skips the sequence. */
+ * that look there are unspecified, gto_kv_commit skips the sequence if one of its new entries would lie there. */
 
 typedef struct gto_decode_ctx gto_decode_ctx;
 

@@ -200,6 +200,12 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(CommitArgs a)
   __shared__ int s_bad;
   if (tid == 0) s_bad = ok ? 0 : 1;
   __syncthreads();
+  if (ok && ch.lead + len > 0) {
+    // the pages of all entries that stay: without one, append has left the token out
+    const int last = (ch.base + ch.lead + len - 1) / a.b.page_size;
+    for (int p = ch.base / a.b.page_size + tid; p <= last; p += kCommitThreads)
+      if (page_of(a.b, s, p * a.b.page_size) < 0) s_bad = 1;
+  }
   if (ok && tid < len) {
     const int32_t* path = a.path_node + static_cast<int64_t>(s) * a.D;
     const int p = path[tid];

@@ -175,3 +175,42 @@ def test_commit_judges_a_batch_by_the_tokens_it_is_told(gto, tokens, want):
     for bad, error in ((-1, ValueError), (1 << 40, ValueError), (c.T + 1, gto.GtoError), ("x", TypeError)):
         with pytest.raises(error):
             gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, new_len, tokens=bad)
+
+
+@pytest.mark.gpu
+def test_a_chunk_without_its_page_is_not_committed(gto):
+    """Append leaves out the tokens whose page the table does not name: the sequence's length may not count them."""
+    step = small_step(gto)
+    step.page_table[1, 1] = -1                                    # entries 16 .. 31 of sequence 1
+    step.begin(torch.tensor([0, 5, 25, 30], dtype=torch.int32, device=DEV))
+    layers_of(step, 30)
+    assert step.status() == 8
+    step.commit()
+    assert step.status() == 8
+    assert step.kv_len.tolist() == [5, 0, 5]
+    step.page_table[1, 1] = 9
+    step.begin(torch.tensor([0, 1, 21, 22], dtype=torch.int32, device=DEV))
+    layers_of(step, 22)
+    step.commit()
+    assert step.status() == 0
+    assert step.kv_len.tolist() == [6, 20, 6]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("missing,length,want", [(2, 0, 33), (2, 1, 34), (3, 0, 33), (3, 2, 35), (2, 2, -5), (1, 0, 33), (1, 1, 34)])
+def test_commit_needs_the_pages_of_the_entries_that_stay_and_no_others(gto, missing, length, want):
+    """A lead of 3 on 30 entries, in pages of 17: entries 30 .. 32 and the accepted nodes' 33, 34, ...; the tree reaches entry 53
+    (page 3); page 2 begins at entry 34."""
+    c = dc.Case([24], [54], 4, 2, 64, 17, "bf16", 21, 3, [21], seed=1, poison=0.0)
+    if missing == 1:
+        c.batch["page_table"][0, 0] = -1          # behind the chunk: attention needs it, commit does not
+    else:
+        c.batch["page_table"][0, missing] = -1
+    path = [[0, -1, -1], [0, -1, -1], [0, 17, -1] if missing == 2 else [0, 1, -1]][length]
+    verdict = dict(accept_len=torch.tensor([length], dtype=torch.int32, device=DEV),
+                   path_node=torch.tensor([path], dtype=torch.int32, device=DEV), token=torch.zeros((1, 4), dtype=torch.int32, device=DEV))
+    new_len = torch.full((1,), -5, dtype=torch.int32, device=DEV)
+    ctx = c.ctx(gto)
+    gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, new_len)
+    assert new_len.tolist() == [want]
+    assert gto.gto_decode_status(ctx) == (8 if want < 0 else 0)
