@@ -41,8 +41,9 @@ typedef enum {
   GTO_ERR_WORKSPACE = 3,   /* workspace allocation failed                                */
   GTO_ERR_CUDA = 4,        /* a CUDA runtime call failed                                 */
   GTO_ERR_NONFINITE = 5,   /* device status: a row's log-sum-exp was not finite          */
-  GTO_ERR_TIMEOUT = 6,     /* device status: a wait inside gto_tree_attention ran out; the
-                              outputs of that call are unspecified                       */
+  GTO_ERR_TIMEOUT = 6,     /* device status: a wait inside gto_tree_attention or gto_verify_tree
+                              ran out; the outputs of that attention are unspecified, the
+                              sequences of that verification have accept_len -1            */
   GTO_ERR_TOO_LARGE = 7,   /* gto_build_tree_noalloc: batch exceeds the fixed scratch    */
   GTO_ERR_BAD_INDEX = 8    /* device status: an index in a caller's table (d2t, a tree's
                               rows, tokens or parents, a path's rows, a page table, the
@@ -375,7 +376,8 @@ typedef struct {
 } gto_draft_tree;
 
 typedef struct {
-  int32_t* accept_len;  /* [S] accepted drafted tokens                                      */
+  int32_t* accept_len;  /* [S] accepted drafted tokens; -1: a wait ran out (GTO_ERR_TIMEOUT), the
+                           sequence's path_node and token are unspecified                   */
   int32_t* path_node;   /* [S, D] their list positions; -1 beyond accept_len                */
   int32_t* token;       /* [S, D+1] their target-vocabulary ids, then the token that follows
                            them (-1 if the last node has no target row); -1 beyond          */
@@ -429,7 +431,9 @@ gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const
  * row is first summed in fp32 with a bound on its error, and again in fp64 where a decision lies
  * within that bound of its border).  A sequence whose visited
  * rows hold NaN or +inf, or nothing but -inf, or whose temperature is negative or not finite,
- * is reported (GTO_ERR_NONFINITE); it keeps what was accepted before and gets the last token -1. */
+ * is reported (GTO_ERR_NONFINITE); it keeps what was accepted before and gets the last token -1.  Where a
+ * CTA of a sequence is not heard of within about two seconds, GTO_ERR_TIMEOUT is reported and the
+ * sequence's accept_len is -1, which gto_kv_commit skips. */
 gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, const void* target,
                            const int32_t* d2t, const float* temperature, const float* u_node,
                            const float* u_bonus, const gto_verdict* out, void* stream);
@@ -439,7 +443,8 @@ gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, cons
  * accept_len[s] (base + n for a sequence without a tree in this batch; untouched for one that is
  * skipped).  batch is the step's, T among it: a sequence that gto_kv_append skipped for lying behind its T
  * tokens is skipped here too.  kv_len_out must not be batch->kv_len, which the whole call reads.  path_node must
- * increase along the path, as gto_verify_tree writes it. */
+ * increase along the path, as gto_verify_tree writes it; a sequence where it does not, or whose accept_len is
+ * negative or above D, is reported and skipped. */
 gto_status gto_kv_commit(gto_decode_ctx* ctx, const gto_batch* batch, const gto_verdict* verdict,
                          const gto_kv_cache* cache, int32_t* kv_len_out, void* stream);
 

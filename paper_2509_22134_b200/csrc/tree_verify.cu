@@ -675,6 +675,9 @@ __global__ void __launch_bounds__(kThreads, kResident) verify_tree_kernel(Verify
     if (tid == 0) atomicOr(a.status, kStatusTimeout);
     asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
     asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+    // no verdict, also where the first CTA has heard of all (it has then written its own and left)
+    if (tid == 0) a.accept_len[s] = -1;
+    return;
   }
   // What the walk did not fill.  (Else a CTA may leave: whatever the others sent it, it has waited for.)
   if (rank == 0) {

@@ -214,3 +214,36 @@ def test_commit_needs_the_pages_of_the_entries_that_stay_and_no_others(gto, miss
     gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, new_len)
     assert new_len.tolist() == [want]
     assert gto.gto_decode_status(ctx) == (8 if want < 0 else 0)
+
+
+@pytest.mark.gpu
+def test_commit_skips_a_sequence_without_a_verdict(gto):
+    """accept_len -1 is what gto_verify_tree leaves where a wait ran out; its path may hold anything."""
+    c = dc.Case([7, 7, 7], [30, 40, 50], 4, 2, 64, 16, "bf16", 6, 3, seed=1, poison=0.0)
+    ctx = c.ctx(gto)
+    verdict = dict(accept_len=torch.tensor([-1, 1, 4], dtype=torch.int32, device=DEV),
+                   path_node=torch.tensor([[0, 1, 2], [2, -1, -1], [0, 1, 2]], dtype=torch.int32, device=DEV),
+                   token=torch.zeros((3, 4), dtype=torch.int32, device=DEV))
+    k, v = c.dk.clone(), c.dv.clone()
+    page, place = (int(x) for x in dec.slots(c.host, 1, 34, 16))
+    to, at = (int(x) for x in dec.slots(c.host, 1, 36, 16))
+    k[page, place], v[page, place] = c.dk[to, at], c.dv[to, at]
+    new_len = torch.full((3,), -5, dtype=torch.int32, device=DEV)
+    gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, new_len)
+    assert gto.gto_decode_status(ctx) == 8
+    assert new_len.tolist() == [-5, 35, -5]
+    assert torch.equal(c.dk, k) and torch.equal(c.dv, v)
+
+
+def test_the_header_names_every_call_whose_waits_can_run_out(repo_root):
+    """The two kernels that raise the status bit belong to these calls."""
+    import os
+    import re
+    src = os.path.join(repo_root, "paper_2509_22134_b200", "csrc")
+    raising = {f for f in os.listdir(src) if f.endswith(".cu") and "atomicOr" in open(os.path.join(src, f)).read()
+               and re.search(r"atomicOr\([^;]*kStatusTimeout", open(os.path.join(src, f)).read())}
+    assert raising == {"tree_attention_tc.cu", "tree_verify.cu"}
+    text = open(os.path.join(repo_root, "include", "gto.h")).read()
+    entry = text[text.index("GTO_ERR_TIMEOUT = 6"):]
+    entry = entry[:entry.index("*/")]
+    assert "gto_tree_attention" in entry and "gto_verify_tree" in entry
