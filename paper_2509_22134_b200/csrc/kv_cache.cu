@@ -187,26 +187,22 @@ constexpr int kCommitBatch = 8;
 __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(CommitArgs a) {
   const int s = blockIdx.x, layer = blockIdx.y, tid = threadIdx.x;
   const Chunk ch = load_chunk(a.b, s);
-  bool behind = false;  // a decrease of q_start, which the CTA of the sequence there reports
-  for (int j = tid; j < s; j += kCommitThreads) behind |= falls(a.b, j);
-  if (__syncthreads_or(behind)) return;
-  if (ch.n == 0 && ch.ok) {
-    if (layer == 0 && tid == 0) a.kv_len_out[s] = ch.len;
-    return;
-  }
-  const int len = ch.ok && ch.nodes > 0 ? a.accept_len[s] : 0;
-  bool ok = ch.ok && len >= 0 && len <= a.D;
+  const int accepted = a.accept_len[s];
+  const int len = ch.ok && ch.nodes > 0 ? accepted : 0;
+  const bool ok = ch.ok && len >= 0 && len <= a.D;
   __shared__ int64_t s_ksrc[kMaxDepth], s_kdst[kMaxDepth], s_vsrc[kMaxDepth], s_vdst[kMaxDepth];
-  __shared__ int s_bad;
-  if (tid == 0) s_bad = ok ? 0 : 1;
-  __syncthreads();
-  if (ok && ch.lead + len > 0) {
-    // the pages of all entries that stay: without one, append has left the token out
-    const int last = (ch.base + ch.lead + len - 1) / a.b.page_size;
-    for (int p = ch.base / a.b.page_size + tid; p <= last; p += kCommitThreads)
-      if (page_of(a.b, s, p * a.b.page_size) < 0) s_bad = 1;
-  }
-  if (ok && tid < len) {
+  bool bad = !ok, behind = false;
+  static_assert(kMaxDepth <= 32, "the first warp looks up the path, the others the rest meanwhile");
+  if (tid >= 32) {
+    // a decrease of q_start, which the CTA of the sequence there reports
+    for (int j = tid - 32; j < s; j += kCommitThreads - 32) behind |= falls(a.b, j);
+    if (ok && ch.lead + len > 0) {
+      // the pages of all entries that stay: without one, append has left the token out
+      const int last = (ch.base + ch.lead + len - 1) / a.b.page_size;
+      for (int p = ch.base / a.b.page_size + tid - 32; p <= last; p += kCommitThreads - 32)
+        bad |= page_of(a.b, s, p * a.b.page_size) < 0;
+    }
+  } else if (ok && tid < len) {
     const int32_t* path = a.path_node + static_cast<int64_t>(s) * a.D;
     const int p = path[tid];
     const int before = tid > 0 ? path[tid - 1] : -1;
@@ -221,11 +217,10 @@ __global__ void __launch_bounds__(kCommitThreads) kv_commit_kernel(CommitArgs a)
       s_vsrc[tid] = p0 * a.c.v_page + r0 * a.c.v_entry;
       s_vdst[tid] = p1 * a.c.v_page + r1 * a.c.v_entry;
     }
-    if (!good) s_bad = 1;
+    bad = !good;
   }
-  __syncthreads();
-  if (s_bad) {
-    if (tid == 0) atomicOr(a.b.status, kStatusBadIndex);
+  if (__syncthreads_or(bad || behind)) {
+    if (!__syncthreads_or(behind) && tid == 0) atomicOr(a.b.status, kStatusBadIndex);
     return;
   }
   if (layer == 0 && tid == 0) a.kv_len_out[s] = ch.base + ch.lead + len;
