@@ -4,7 +4,9 @@ for the calls of a decoding step, where microseconds count.
 The functions carry the names of the C entry points (include/gto.h) and take torch
 tensors for device buffers; PyTorch supplies device memory and streams, every step of
 the pass runs in the library's kernels.  Importing this module loads the library and
-raises if it has not been built - there is no fallback path.
+raises if it has not been built - there is no fallback path.  The extension is loaded by the
+first decoding context (gto_decode_create), which raises if it has not been built for this
+Python and PyTorch; the training pass does without it.
 """
 from __future__ import annotations
 
@@ -28,11 +30,22 @@ if not os.path.exists(LIB_PATH):
         f"{LIB_PATH} is missing: build it with `python -m paper_2509_22134_b200.build` "
         "(the GTO pass has no CPU or PyTorch fallback)")
 _lib = ctypes.CDLL(LIB_PATH)
-try:
-    from . import _gto_decode as _native
-except ImportError as e:
-    raise RuntimeError("_gto_decode.so is missing or does not fit this Python: build it with "
-                       "`python -m paper_2509_22134_b200.build`") from e
+_native = None  # the extension, from the first decoding context on
+
+
+def _load_native():
+    global _native
+    if _native is None:
+        from .build import extension_key
+        advice = "build it with `python -m paper_2509_22134_b200.build`"
+        try:
+            from . import _gto_decode
+        except ImportError as e:
+            raise RuntimeError(f"_gto_decode.so is missing or cannot be loaded ({e}): {advice}") from e
+        if _gto_decode.built_for != extension_key():
+            raise RuntimeError(f"_gto_decode.so was built for {_gto_decode.built_for}, this is {extension_key()}: {advice}")
+        _native = _gto_decode
+    return _native
 
 
 class gto_config(ctypes.Structure):
@@ -387,6 +400,7 @@ def _stream_of(ctx: DecodeCtx, stream) -> int:
 
 
 def gto_decode_create(cfg: gto_decode_config, device: int = 0) -> DecodeCtx:
+    _load_native()
     h = _vp()
     _check(_lib.gto_decode_create(ctypes.byref(h), ctypes.byref(cfg), device), "gto_decode_create")
     return DecodeCtx(h.value, gto_decode_config.from_buffer_copy(cfg), device)

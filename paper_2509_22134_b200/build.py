@@ -12,6 +12,7 @@ CSRC = os.path.join(HERE, "csrc")
 OBJ = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgto.so")
 EXT = os.path.join(HERE, "_gto_decode.so")
+EXT_KEY = os.path.join(OBJ, "_gto_decode.key")  # what EXT was built for
 SOURCES = ["gto_api.cu", "row_reduce.cu", "tree_build.cu", "tree_reward.cu", "surrogate_grad.cu",
            "build_tree_noalloc.cu", "token_loss.cu", "decode_api.cu", "kv_cache.cu", "tree_verify.cu",
            "tree_attention_simt.cu", "tree_attention_tc.cu"]
@@ -29,6 +30,22 @@ def _stale(out: str, deps: list[str]) -> bool:
         return True
     t = os.path.getmtime(out)
     return any(os.path.getmtime(d) > t for d in deps)
+
+
+def extension_key() -> str:
+    """What the extension is compiled against: it is stale, and not loaded, under another Python or PyTorch."""
+    import sysconfig
+    import torch
+    return f"{sysconfig.get_config_var('SOABI')} torch {torch.__version__}"
+
+
+def _extension_stale(deps: list[str]) -> bool:
+    try:
+        with open(EXT_KEY) as f:
+            key = f.read()
+    except OSError:
+        return True
+    return key != extension_key() or _stale(EXT, deps)
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
@@ -63,7 +80,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
         if r.returncode != 0:
             raise RuntimeError(f"link failed:\n{r.stderr}")
     src = os.path.join(CSRC, "decode_binding.cpp")
-    if force or _stale(EXT, [src, headers[-1]]):
+    if force or _extension_stale([src, headers[-1]]):
         import sysconfig
         import torch
         inc = os.path.join(os.path.dirname(torch.__file__), "include")
@@ -71,10 +88,13 @@ def build(force: bool = False, verbose: bool = False) -> str:
                             os.path.join(inc, "torch", "csrc", "api", "include"), "-I",
                             sysconfig.get_paths()["include"],
                             f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+                            f'-DGTO_BUILT_FOR="{extension_key()}"',
                             LIB, "-Wl,-rpath,$ORIGIN", "-L", os.path.join(os.path.dirname(inc), "lib"),
                             "-ltorch_python", "-ltorch_cpu", "-lc10"], capture_output=True, text=True)
         if r.returncode != 0:
             raise RuntimeError(f"g++ failed on {src}:\n{r.stderr}")
+        with open(EXT_KEY, "w") as f:
+            f.write(extension_key())
     return LIB
 
 

@@ -325,4 +325,11 @@ PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_gto_decode", nullptr, -1, kMetho
 
 }  // namespace
 
-PyMODINIT_FUNC PyInit__gto_decode() { return PyModule_Create(&kModule); }
+PyMODINIT_FUNC PyInit__gto_decode() {
+  PyObject* m = PyModule_Create(&kModule);
+  if (m && PyModule_AddStringConstant(m, "built_for", GTO_BUILT_FOR) != 0) {
+    Py_DECREF(m);
+    return nullptr;
+  }
+  return m;
+}
