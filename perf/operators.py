@@ -208,16 +208,6 @@ def _config(gto, case, size, **kw):
                                   max_pages=size["max_pages"], dtype=case["dtype"], g=case["g"], D=case["D"], **kw)
 
 
-class _Context:
-    """The library's context, as a program keeps it for as long as it decodes."""
-
-    def __init__(self, gto, cfg):
-        self.gto, self.handle = gto, gto.gto_decode_create(cfg, torch.cuda.current_device())
-
-    def __del__(self):
-        self.gto.gto_decode_destroy(self.handle)
-
-
 # ------------------------------------------------------------------ inputs
 def _inputs(case, seed):
     gen = _gen(seed)
@@ -299,14 +289,15 @@ def prepare(case, seed):
                           flags=gto.GTO_DECODE_ROPE_INTERLEAVED if case["inter"] else 0)
         else:
             cfg = _config(gto, case, s["size"])
-        s["ctx"] = _Context(gto, cfg)
+        # the library's context, as a program keeps it for as long as it decodes (it frees itself)
+        s["ctx"] = gto.gto_decode_create(cfg, torch.cuda.current_device())
     return s
 
 
 # ------------------------------------------------------------------ the library's calls
 def _run_own(s):
     from paper_2509_22134_b200 import binding as gto
-    case, op, ctx = s["case"], s["case"]["op"], s["ctx"].handle
+    case, op, ctx = s["case"], s["case"]["op"], s["ctx"]
     if op == "append":
         hq, hkv, x = case["hq"], case["hkv"], s["qkv"]
         gto.gto_kv_append(ctx, s["batch"], x[:, :hq], x[:, hq:hq + hkv], x[:, hq + hkv:], s["q_out"], s["k_cache"],
