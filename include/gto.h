@@ -356,7 +356,8 @@ typedef struct {
 
 /* Paged keys and values.  Element (layer, page, entry, head, :) starts at the sum of the
  * indices times the strides; the head_dim values of a head are contiguous.  Strides count
- * elements, multiples of 16 bytes. */
+ * elements, multiples of 16 bytes.  No two elements share memory, and the token arrays of a call share none
+ * with the cache. */
 typedef struct {
   void* k;
   void* v;
@@ -411,7 +412,7 @@ gto_status gto_kv_append(gto_decode_ctx* ctx, const gto_batch* batch, const gto_
  * the tree and the nodes in row a of node_mask.  A row that sees nothing gives zeros.  q as in
  * gto_kv_append; out: dense [T, n_q_heads, head_dim]; lse ([T, n_q_heads] fp32 or NULL) receives
  * the log-sum-exp of the row's scaled scores, -inf for a row that sees nothing.  Rows of tokens
- * that belong to no sequence are left as they were.  out must not overlap q. */
+ * that belong to no sequence are left as they were.  out and lse overlap neither q nor each other. */
 gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const gto_kv_cache* cache,
                               const void* q, int64_t q_stride, void* out, float* lse, void* stream);
 
@@ -433,7 +434,8 @@ gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const
  * rows hold NaN or +inf, or nothing but -inf, or whose temperature is negative or not finite,
  * is reported (GTO_ERR_NONFINITE); it keeps what was accepted before and gets the last token -1.  Where a
  * CTA of a sequence is not heard of within about two seconds, GTO_ERR_TIMEOUT is reported and the
- * sequence's accept_len is -1, which gto_kv_commit skips. */
+ * sequence's accept_len is -1, which gto_kv_commit skips.  The arrays of *out overlap neither one another
+ * nor what the call reads. */
 gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, const void* target,
                            const int32_t* d2t, const float* temperature, const float* u_node,
                            const float* u_bonus, const gto_verdict* out, void* stream);
@@ -442,7 +444,8 @@ gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, cons
  * to base + lead + j for j < accept_len[s], in all layers, and kv_len_out[s] = base + lead +
  * accept_len[s] (base + n for a sequence without a tree in this batch; untouched for one that is
  * skipped).  batch is the step's, T among it: a sequence that gto_kv_append skipped for lying behind its T
- * tokens is skipped here too.  kv_len_out must not be batch->kv_len, which the whole call reads.  path_node must
+ * tokens is skipped here too.  kv_len_out overlaps neither batch->kv_len, which the whole call reads, nor
+ * another table of the batch or the verdict.  path_node must
  * increase along the path, as gto_verify_tree writes it; a sequence where it does not, or whose accept_len is
  * negative or above D, is reported and skipped. */
 gto_status gto_kv_commit(gto_decode_ctx* ctx, const gto_batch* batch, const gto_verdict* verdict,

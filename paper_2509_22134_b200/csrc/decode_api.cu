@@ -1,5 +1,6 @@
 // C ABI of the decoding step: contexts, argument checks, launch sequencing.
 #include <cmath>
+#include <initializer_list>
 #include <new>
 
 #include <nvtx3/nvToolsExt.h>
@@ -43,6 +44,17 @@ bool table(const void* p, size_t n) { return p != nullptr && aligned(p, n); }
 bool overlap(const void* a, size_t na, const void* b, size_t nb) {
   const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
   return x < y + nb && y < x + na;
+}
+
+// Whether an output lies over one of several arrays.
+struct Array {
+  const void* p;
+  size_t bytes;
+};
+bool over_any(Array out, std::initializer_list<Array> in) {
+  for (const Array& x : in)
+    if (x.p && overlap(out.p, out.bytes, x.p, x.bytes)) return true;
+  return false;
 }
 
 // Bytes a token array of T rows spans.
@@ -251,8 +263,9 @@ gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const
   const int64_t q_row = c.n_q_heads * static_cast<int64_t>(c.head_dim) * e;
   if (!table(q, 16) || !table(out, 16) || (q_stride * e) % 16 || q_stride * e < q_row || (lse && !aligned(lse, 4)))
     return GTO_ERR_INVALID_ARG;
-  if (overlap(q, span(a.b.T, q_stride * e, q_row), out, static_cast<size_t>(a.b.T) * q_row))
-    return GTO_ERR_INVALID_ARG;
+  const Array rows{q, span(a.b.T, q_stride * e, q_row)}, outs{out, static_cast<size_t>(a.b.T) * q_row};
+  if (over_any(outs, {rows})) return GTO_ERR_INVALID_ARG;
+  if (lse && over_any({lse, sizeof(float) * a.b.T * c.n_q_heads}, {rows, outs})) return GTO_ERR_INVALID_ARG;
   a.q = static_cast<const char*>(q);
   a.q_stride = q_stride * e;
   a.out = static_cast<char*>(out);
@@ -290,6 +303,15 @@ gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, cons
   const bool ctx_rows = (c.flags & GTO_DECODE_CONTEXT_ROWS) != 0;
   if (ctx_rows && c.g > 0 && (!table(tree->node_depth, 4) || !table(tree->node_slot, 4)))
     return GTO_ERR_INVALID_ARG;
+  const size_t S = tree->S, word = sizeof(int32_t), nodes = word * S * c.g;
+  const size_t target_rows = ctx_rows ? 1 + static_cast<size_t>(c.D - 1) * c.k : 1 + static_cast<size_t>(c.g);
+  const Array outs[3] = {{out->accept_len, word * S}, {out->path_node, word * S * c.D}, {out->token, word * S * (c.D + 1)}};
+  for (int i = 0; i < 3; ++i)
+    if (over_any(outs[i], {outs[(i + 1) % 3], {tree->node_token, nodes}, {tree->node_parent, nodes},
+                           {ctx_rows ? tree->node_depth : nullptr, nodes}, {ctx_rows ? tree->node_slot : nullptr, nodes},
+                           {tree->n_nodes, word * S}, {target, S * target_rows * c.V_target * gto::elem_bytes(c.logit_dtype)},
+                           {d2t, word * c.V_draft}, {temperature, word * S}, {u_node, nodes}, {u_bonus, word * S}}))
+      return GTO_ERR_INVALID_ARG;
   gto::VerifyArgs a{};
   a.S = tree->S;
   a.g = c.g;
@@ -333,7 +355,10 @@ gto_status gto_kv_commit(gto_decode_ctx* ctx, const gto_batch* batch, const gto_
   if (a.b.S == 0) return GTO_OK;
   if (!verdict || !table(verdict->accept_len, 4) || !table(verdict->path_node, 4) || !table(kv_len_out, 4))
     return GTO_ERR_INVALID_ARG;
-  if (overlap(kv_len_out, sizeof(int32_t) * a.b.S, batch->kv_len, sizeof(int32_t) * a.b.S))
+  const size_t word = sizeof(int32_t), S = a.b.S;
+  if (over_any({kv_len_out, word * S}, {{batch->kv_len, word * S}, {batch->q_start, word * (S + 1)}, {batch->n_nodes, word * S},
+                                        {batch->page_table, word * S * ctx->cfg.max_pages}, {verdict->accept_len, word * S},
+                                        {verdict->path_node, word * S * ctx->cfg.D}}))
     return GTO_ERR_INVALID_ARG;
   a.accept_len = verdict->accept_len;
   a.path_node = verdict->path_node;

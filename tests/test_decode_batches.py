@@ -247,3 +247,56 @@ def test_the_header_names_every_call_whose_waits_can_run_out(repo_root):
     entry = text[text.index("GTO_ERR_TIMEOUT = 6"):]
     entry = entry[:entry.index("*/")]
     assert "gto_tree_attention" in entry and "gto_verify_tree" in entry
+
+
+# ------------------------------------------------------------------ outputs over what a call reads
+
+def refused(gto, ctx, call):
+    before = gto.gto_decode_launch_count(ctx)
+    with pytest.raises(gto.GtoError) as e:
+        call()
+    assert e.value.code == 1 and gto.gto_decode_launch_count(ctx) == before
+
+
+@pytest.mark.gpu
+def test_commit_refuses_lengths_over_a_table_it_reads(gto):
+    c = dc.Case([7, 7, 7], [30, 40, 50], 4, 2, 64, 16, "bf16", 6, 3, [6, 6, 6], seed=1, poison=0.0)
+    ctx = c.ctx(gto)
+    i32 = dict(dtype=torch.int32, device=DEV)
+    verdict = dict(accept_len=torch.zeros(3, **i32), path_node=torch.zeros((3, 3), **i32), token=torch.zeros((3, 4), **i32))
+    for over in (c.batch["kv_len"], c.batch["q_start"][:3], c.batch["q_start"][1:], c.batch["n_nodes"], verdict["accept_len"],
+                 c.batch["page_table"].view(-1)[2:5], verdict["path_node"].view(-1)[4:7]):
+        refused(gto, ctx, lambda: gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, over))
+    gto.gto_kv_commit(ctx, c.batch, verdict, c.dk, c.dv, torch.zeros(3, **i32))
+    assert gto.gto_decode_status(ctx) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_attention_refuses_an_lse_over_queries_or_outputs(gto, dtype):
+    c = dc.Case([7, 7], [30, 40], 4, 2, 64, 16, dtype, seed=1, poison=0.0)
+    ctx = c.ctx(gto)
+    out = torch.zeros_like(c.dq)
+    for over in (c.dq, out):
+        lse = over.view(-1).view(torch.float32)[:c.T * 4].view(c.T, 4)
+        refused(gto, ctx, lambda: gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=lse))
+
+
+@pytest.mark.gpu
+def test_verify_refuses_a_verdict_over_what_it_reads(gto):
+    cfg = gto.make_decode_config(S=3, g=6, D=3, V_draft=512, V_target=512, logit_dtype="f32")
+    ctx = gto.gto_decode_create(cfg, 0)
+    i32, f32 = dict(dtype=torch.int32, device=DEV), dict(device=DEV)
+    tree = dict(node_token=torch.zeros((3, 6), **i32), node_parent=torch.full((3, 6), -1, **i32), n_nodes=torch.full((3,), 6, **i32))
+    target, u = torch.zeros((3, 7, 512), **f32), torch.zeros((3, 6), **f32)
+    temperature, bonus = torch.ones(3, **f32), torch.zeros(3, **f32)
+    good = gto.alloc_verdict(cfg, DEV)
+    call = lambda out: gto.gto_verify_tree(ctx, tree, target, None, temperature, u, bonus, out)
+    as_i32 = lambda t, n: t.view(-1).view(torch.int32)[:n]
+    for name, n, shape in (("accept_len", 3, (3,)), ("path_node", 9, (3, 3)), ("token", 12, (3, 4))):
+        for over in (tree["node_token"], tree["node_parent"], tree["n_nodes"], target, u, temperature, bonus,
+                     *(good[m] for m in good if m != name)):
+            if over.numel() >= n:
+                refused(gto, ctx, lambda: call({**good, name: as_i32(over, n).view(shape)}))
+    call(good)
+    assert gto.gto_decode_status(ctx) == 0
