@@ -412,7 +412,9 @@ gto_status gto_kv_append(gto_decode_ctx* ctx, const gto_batch* batch, const gto_
  * the tree and the nodes in row a of node_mask.  A row that sees nothing gives zeros.  q as in
  * gto_kv_append; out: dense [T, n_q_heads, head_dim]; lse ([T, n_q_heads] fp32 or NULL) receives
  * the log-sum-exp of the row's scaled scores, -inf for a row that sees nothing.  Rows of tokens
- * that belong to no sequence are left as they were.  out and lse overlap neither q nor each other. */
+ * that belong to no sequence are left as they were.  out and lse overlap neither q nor each other.  A
+ * value (of v) that is not finite can make the outputs of a row that sees it not finite in all dimensions,
+ * not in its own alone; rows that do not see it, and every lse, are not touched by it. */
 gto_status gto_tree_attention(gto_decode_ctx* ctx, const gto_batch* batch, const gto_kv_cache* cache,
                               const void* q, int64_t q_stride, void* out, float* lse, void* stream);
 

@@ -102,6 +102,7 @@ struct Tail {
   Chunk chunk;                  // of that sequence
   uint32_t tmem;
   int abort;
+  uint32_t lost[8];             // softmax warps: rows (lanes) that see a value that is not finite
 };
 
 // ------------------------------------------------------------------ instructions
@@ -773,6 +774,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       const int step = dual ? 1 : 2, j0 = dual ? 0 : st;
       const int first_masked = max(it.common / kTile, it.t0);  // tiles from here on are masked
       float m = -INFINITY, l = 0.f;  // reference and sum
+      if (lane == 0) t.lost[warp] = 0;
       if (it.alike && !__any_sync(kFull, valid)) {
         // a warp of rows that do not exist: their scores and weights may stay what they are
         for (int j = j0; j < nt && ok; j += step, ++seen) {
@@ -795,7 +797,7 @@ __global__ void __launch_bounds__(kThreads, 1)
             *reinterpret_cast<uint4*>(v + (q / 8 % L::kHalves) * L::kHalfBytes + (n + q / (8 * L::kHalves)) * 128 +
                                       q % 8 * 16) = make_uint4(0, 0, 0, 0);
           // Entries that some rows do not see must be finite for those: where they are not they
-          // become 0, and the rows that see them get NaN weights.  Every warp looks at all of them,
+          // become 0, and the rows that see them get NaN in the end.  Every warp looks at all of them,
           // and nobody writes before all have looked.
           uint32_t bad0 = 0, bad1 = 0;
           if (!it.alike) {
@@ -844,12 +846,14 @@ __global__ void __launch_bounds__(kThreads, 1)
                 see |= static_cast<uint32_t>(bits);
               }
             }
-            const uint32_t nan = c ? bad1 : bad0;
-#pragma unroll
-            for (int q = 0; q < 32; ++q) {
-              if (!(see >> q & 1)) x[c][q] = 0xff800000u;
-              else if (nan >> q & 1) x[c][q] = 0x7fffffffu;
+            const uint32_t bad = c ? bad1 : bad0;
+            if (bad != 0) {
+              const uint32_t rows = __ballot_sync(kFull, (see & bad) != 0);
+              if (lane == 0) t.lost[warp] |= rows;
             }
+#pragma unroll
+            for (int q = 0; q < 32; ++q)
+              if (!(see >> q & 1)) x[c][q] = 0xff800000u;
           }
         };
         auto max_of = [](const uint32_t (&y)[32]) {
@@ -942,6 +946,9 @@ __global__ void __launch_bounds__(kThreads, 1)
         if (!ok) break;
         tc_after();
       }
+      // a sum below zero (or -0) says that the row's output is lost; its magnitude is the sum
+      __syncwarp();
+      if (t.lost[warp] >> lane & 1) l = -l;
       const bool join = !dual && nt > 1;
       float w0 = 1.f, w1 = 0.f;
       if (join) {
@@ -963,7 +970,8 @@ __global__ void __launch_bounds__(kThreads, 1)
         const float ref = mm == -INFINITY ? 0.f : mm;
         w0 = ex2_approx(m - ref);
         w1 = ex2_approx(mo - ref);
-        l = l * w0 + lo * w1;
+        const float sum = fabsf(l) * w0 + fabsf(lo) * w1;
+        l = signbit(l) || signbit(lo) ? -sum : sum;
         m = mm;
       } else if (!mine) {
         continue;
@@ -971,7 +979,8 @@ __global__ void __launch_bounds__(kThreads, 1)
       const bool whole = it.whole();
       const int64_t tok = ch.q0 + i;
       const int h = it.kvh * geo.group + static_cast<int>(row) - (i - it.first) * geo.group;
-      const float inv = l > 0.f ? 1.f / l : (l == 0.f ? 0.f : NAN);
+      const float sum = fabsf(l);
+      const float inv = signbit(l) ? NAN : sum > 0.f ? 1.f / sum : (sum == 0.f ? 0.f : NAN);
       const int64_t slot = 2 * static_cast<int64_t>(blockIdx.x) + (it.t0 == 0 ? 1 : 0);
       uint4* out = reinterpret_cast<uint4*>(a.out + (tok * a.n_q_heads + h) * static_cast<int64_t>(DH * 2));
       float4* part = p.part + slot * (DH / 4) * kBlock + r;
@@ -1019,7 +1028,7 @@ __global__ void __launch_bounds__(kThreads, 1)
       if (valid) {
         if (!whole) p.part_ml[slot * kBlock + r] = make_float2(m, l);
         else if (a.lse != nullptr)
-          a.lse[tok * a.n_q_heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.6931471805599453f;
+          a.lse[tok * a.n_q_heads + h] = sum == 0.f ? -INFINITY : (m + log2f(sum)) * 0.6931471805599453f;
       }
     }
   }
@@ -1072,9 +1081,9 @@ __global__ void __launch_bounds__(kJoinThreads) attention_join_kernel(const __gr
     const float2 ml = lane < n_rows ? p.part_ml[slot(i) * kBlock + first_row + lane] : make_float2(-INFINITY, 0.f);
     const float top = fmaxf(m, ml.x);
     const float ref = top == -INFINITY ? 0.f : top;
-    l = l * ex2_approx(m - ref) + ml.y * ex2_approx(ml.x - ref);
+    l = l * ex2_approx(m - ref) + fabsf(ml.y) * ex2_approx(ml.x - ref);
     m = top;
-    s_w[i][lane] = ml.x;
+    s_w[i][lane] = signbit(ml.y) ? NAN : ml.x;  // (a row whose output is lost)
   }
   s_m[warp][lane] = m;
   s_l[warp][lane] = l;

@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import decode_cases as dc
+from oracle import decode_oracle as dec
 
 pytestmark = pytest.mark.gpu
 
@@ -56,3 +57,40 @@ def test_a_flat_tail_behind_one_large_score_is_kept(gto, n, gap, dh, dtype):
     assert torch.all(err <= want * (3 * dc.HALF_STEP[dtype] + 2.0 ** -18 + 4 * tiles * 2.0 ** -24)), float((err / want).max())
     err = (lse.double().cpu() - (top + np.log1p(w * (n - 1)))).abs()
     assert torch.all(err <= 2.0 ** -18 + tiles * 2.0 ** -25 + 2.0 ** -22 * top), float(err.max())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("q_lens,kv_lens,g,hq,dh", [
+    ([13], [70], 12, 4, 64),                     # one block, both streams on its tiles
+    ([13], [4000], 12, 8, 128),                  # cut into many parts
+    ([13] * 40, [1500] * 40, 12, 8, 64),
+    ([129], [300], 128, 8, 128),                 # two row tiles, two words of a mask
+    ([70], [90], 0, 16, 64),                     # a prompt
+])
+def test_a_value_that_is_not_finite_spoils_no_lse_and_no_row_that_does_not_see_it(gto, q_lens, kv_lens, g, hq, dh, bad, dtype):
+    c = dc.Case(q_lens, kv_lens, hq, 2, dh, 16, dtype, g, 5, seed=len(q_lens) + g, poison=0.0)
+    scale = dh ** -0.5
+    want, want_z, spread = c.attention_on_device(scale)
+    sees = np.zeros(c.T, bool)
+    for s in range(c.S):
+        n, L = q_lens[s], kv_lens[s]
+        hit = 5 if g else n - 20                               # entry L - n + lead + 5, or the prompt's 20th from its end
+        e = L - g + hit if g else L - n + hit
+        page, place = dec.slots(c.host, s, [e], c.page)
+        c.v[page, place] = bad
+        q0 = int(c.host["q_start"][s])
+        if g:
+            sees[q0 + n - g:q0 + n] = c.host["node_mask"][s][:, hit]
+        else:
+            sees[q0 + hit:q0 + n] = True
+    c.dv = c.pool(c.v)
+    ctx = c.ctx(gto, softmax_scale=scale)
+    out, lse = torch.zeros_like(c.dq), torch.zeros((c.T, hq), device=DEV)
+    gto.gto_tree_attention(ctx, c.batch, c.dq, c.dk, c.dv, out, lse=lse)
+    assert gto.gto_decode_status(ctx) == 0
+    got, z = out.double().cpu().numpy()[:c.n], lse.double().cpu().numpy()[:c.n]
+    assert np.all(np.abs(z - want_z[:c.n]) <= 1e-4)             # dh products of at most about 10 in fp32: 128 * 10 * 2^-23 / 11
+    blind = ~sees[:c.n]
+    assert np.all(np.abs(got[blind] - want[:c.n][blind]) <= spread[:c.n][blind] * (dc.HALF_STEP[dtype] * 2 + 1e-3))
+    assert not np.isfinite(got[sees[:c.n]]).any()
