@@ -34,7 +34,10 @@ __device__ int find_unit(const BatchArgs& b, int64_t unit, F units, int64_t* res
   __shared__ int s_found, s_fall;
   __shared__ int64_t s_rest;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  if (tid == 0) s_found = -1;
+  if (tid == 0) {
+    s_found = -1;
+    s_fall = b.S;
+  }
   int64_t before = 0;
   for (int s0 = 0; s0 < b.S; s0 += kThreads) {
     const int s = s0 + tid;
@@ -58,12 +61,10 @@ __device__ int find_unit(const BatchArgs& b, int64_t unit, F units, int64_t* res
       if (lane == 31) s_scan[warp] = run;
     };
     scan();
-    const bool last = __syncthreads_or(fall);
+    if (fall) atomicMin(&s_fall, s);
+    __syncthreads();
+    const bool last = s_fall < b.S;
     if (last) {  // once more without the sequences that are skipped
-      if (tid == 0) s_fall = b.S;
-      __syncthreads();
-      if (fall) atomicMin(&s_fall, s);
-      __syncthreads();
       if (s >= s_fall) n = 0;
       scan();
       __syncthreads();
