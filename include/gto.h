@@ -400,7 +400,7 @@ gto_status gto_decode_destroy(gto_decode_ctx* ctx);
  * square and multiplied by the weights.  Then the pair (x_i, x_{i + rope_dims/2}) is rotated by
  * the angle position * inv_freq[i] (inv_freq: [rope_dims/2] fp64; the angle is formed in fp64,
  * so that far positions keep their phase).  Everything in fp32, rounded once.  Values are
- * copied.  Two sequences must not own the same cache entry. */
+ * copied.  No two tokens of the batch may own the same cache entry. */
 gto_status gto_kv_append(gto_decode_ctx* ctx, const gto_batch* batch, const gto_kv_cache* cache,
                          const void* q, int64_t q_stride, const void* k, int64_t k_stride,
                          const void* v, int64_t v_stride, void* q_out, const double* inv_freq,

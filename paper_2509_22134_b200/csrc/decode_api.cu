@@ -53,7 +53,7 @@ struct Array {
 };
 bool over_any(Array out, std::initializer_list<Array> in) {
   for (const Array& x : in)
-    if (x.p && overlap(out.p, out.bytes, x.p, x.bytes)) return true;
+    if (x.p && x.bytes && overlap(out.p, out.bytes, x.p, x.bytes)) return true;
   return false;
 }
 

@@ -300,3 +300,21 @@ def test_verify_refuses_a_verdict_over_what_it_reads(gto):
                 refused(gto, ctx, lambda: call({**good, name: as_i32(over, n).view(shape)}))
     call(good)
     assert gto.gto_decode_status(ctx) == 0
+
+
+@pytest.mark.gpu
+def test_an_array_without_elements_lies_over_nothing(gto):
+    """Without trees the node arrays have no elements: where they point does not matter."""
+    import ctypes
+    cfg = gto.make_decode_config(S=2, g=0, D=1, V_draft=64, V_target=64, logit_dtype="f32")
+    ctx = gto.gto_decode_create(cfg, 0)
+    out = gto.alloc_verdict(cfg, DEV)
+    buf = torch.zeros(4, dtype=torch.int32, device=DEV)
+    target, t, u = torch.zeros((2, 1, 64), device=DEV), torch.zeros(2, device=DEV), torch.zeros(2, device=DEV)
+    tree = gto.gto_draft_tree(2, buf.data_ptr() + 4, buf.data_ptr() + 4, None, None, None)
+    verdict = gto.gto_verdict(buf.data_ptr(), out["path_node"].data_ptr(), out["token"].data_ptr())
+    code = gto._lib.gto_verify_tree(ctypes.c_void_p(ctx.handle), ctypes.byref(tree), ctypes.c_void_p(target.data_ptr()), None,
+                                    ctypes.c_void_p(t.data_ptr()), ctypes.c_void_p(buf.data_ptr() + 4), ctypes.c_void_p(u.data_ptr()),
+                                    ctypes.byref(verdict), ctypes.c_void_p(torch.cuda.current_stream().cuda_stream))
+    assert code == 0 and gto.gto_decode_status(ctx) == 0
+    assert buf[:2].tolist() == [0, 0] and out["token"][:, 0].tolist() == [0, 0]
