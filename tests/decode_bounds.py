@@ -7,7 +7,8 @@ The errors counted (e: cache entry, d: dimension, half: half a step of the type,
   weight      the exponential errs by 2^-22, the sums (of tens to hundreds of partial sums) by less than 2^-21: 2^-20 in all.
   16 bits     weights are rounded to the type, independently: |error| <= half p_e, and the sum of n independent errors passes
               7 half sqrt(sum (p_e v_e)^2) with probability 2 exp(-49/2) = 5e-11 (Hoeffding); half sum p_e |v_e| at most.
-  result      rounded once: half |out|.
+  result      rounded once: half |out|, and where the type's numbers are subnormal half of their step (fp16: numbers below 2^-14
+              lie 2^-24 apart, whatever their size, so that rounding one errs by up to 2^-25).
 A first-order change of scores by s_e changes out by sum_e p_e s_e (v_e - out) and the log-sum-exp by sum_e p_e s_e.
 
 Over all results the root mean square is held too: the terms but the last are at least 4 standard deviations each, and
@@ -64,7 +65,7 @@ def expected(c, scale, device="cpu", drop=None, weights=None, dtype=None):
         r["lse"].append(lse.T)
         r["lse_tol"].append((p * step).sum(2).T + 2.0 ** -19 + 2.0 ** -22 * torch.where(torch.isinf(lse), 0.0, lse.abs()).T)
     r = {n: torch.cat(x).cpu().numpy() for n, x in r.items()}
-    r["half"] = half
+    r["half"], r["subnormal"] = half, 2.0 ** -25 if c.dtype == "f16" else 1e-30
     return r
 
 
@@ -72,7 +73,7 @@ def misses(want, out, lse):
     """What is wrong with results out [n, hq, dh] and lse [n, hq] (fp64 numpy): a list of texts, empty where nothing is."""
     bad = []
     err = np.abs(out - want["out"])
-    tol = want["rest"] + want["half"] * np.abs(want["out"]) + 1e-30
+    tol = want["rest"] + want["half"] * np.abs(want["out"]) + want["subnormal"]
     if not np.all(err <= tol):                                     # (NaN too)
         part = np.nan_to_num(err / tol, nan=np.inf)
         bad.append("out: %.3g of its tolerance at %s" % (part.max(), np.unravel_index(np.argmax(part), part.shape)))
