@@ -305,7 +305,8 @@ gto_status gto_kernel_times(gto_ctx* ctx, void* stream, double* total_ms, int64_
  * below the last of them (or, with lead = 0, below entry base - 1).
  * Entry t of sequence s lies in place t % page_size of page page_table[s][t / page_size].
  *
- * The functions take a gto_decode_ctx, which owns the workspace and a status word.  Calls
+ * The functions take a gto_decode_ctx, which owns the workspace (for bf16 / fp16 caches with heads of 64 or 128 about
+ * 20 / 39 MB, whatever the other sizes are) and a status word.  Calls
  * through one context share them: order them (one stream, events), and give every stream or
  * captured graph that may run at the same time a context of its own.  The calls can be
  * captured into a CUDA graph, which the context has to outlive; lengths, tables and trees are

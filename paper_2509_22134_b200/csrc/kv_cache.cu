@@ -3,12 +3,12 @@
 // bounds them: append reads and writes (n_q + 2 n_kv) * head_dim values a token once, commit reads
 // and writes 2 * n_kv * head_dim values an accepted token and layer once.
 //
-// Measured, heads of 128: eight prompts of up to 4000 tokens, 40 query and 40 key heads, 186 us (96 % of the
-// copy rate); 64 trees of 61 tokens, 32 and 8 heads, 24.7 us, of which 14.9 are the bytes and the rest
+// Measured, heads of 128: eight prompts of up to 4000 tokens, 40 query and 40 key heads, 185 us (97 % of the
+// copy rate); 64 trees of 61 tokens, 32 and 8 heads, 25.1 us, of which 14.9 are the bytes and the rest
 // the chain place -> position -> rotation of three waves of CTAs.  Asking for the rows before that
 // chain cost more in registers than it hid (26 to 32 us), prefetching them into L2 too (26 us);
 // 42 registers a thread for a wave less gave 181 and 24.9 us, and 4.0 instead of 3.6 for one token.
-// Commit: 64 sequences, 32 layers 13.9 us (9.1 for the bytes).
+// Commit: 64 sequences, 32 layers 13.8 to 14.2 us (9.1 for the bytes).
 #include "decode_common.cuh"
 
 namespace gto {

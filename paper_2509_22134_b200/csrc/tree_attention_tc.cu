@@ -31,15 +31,16 @@
 // what is below 2^-36 of it is lost.
 //
 // What bounds it (32 query heads, 8 key heads of 128; B200 at 1.7 to 1.97 GHz).  Single tokens: the copies;
-// 128 sequences of 1500 to 6000 entries take 341 us, 5.8 TB/s.  Trees and prompts: a step of 64
+// 128 sequences of 1500 to 6000 entries take 340 to 370 us by the board, 5.4 to 5.8 TB/s (83 to 90 % of the
+// copy rate; the clock falls to 1.5 to 1.6 GHz).  Trees and prompts: a step of 64
 // entries on 256 rows takes 2240 to 2460 cycles, where the matrix instructions need 1280 (a score
 // product of N = 64 reads 6 KB of operands from shared memory in 48 cycles, which is all that it
 // gives, in place of the 32 that the product would need) and the exponentials 1024: a stream's own
 // chain (scores to registers and their maximum 500, exponentials 1180 where two warps of a scheduler
 // have them at once, waits and hand-overs 700) is longer than either.  32 trees of 61 tokens on 1000 to 4000
-// entries take 131 us, four prompts of up to 2048 tokens on up to 6000 cached ones 376 us
-// (810 TFLOP/s of the products that are not masked).  One token of one sequence on 8000 entries takes
-// 20.0 us: 3 until the span is known, 10 for the tiles, 6 for the join.
+// entries take 125 to 131 us, four prompts of up to 2048 tokens on up to 6000 cached ones 364 to 376 us
+// (810 to 840 TFLOP/s of the products that are not masked).  One token of one sequence on 8000 entries takes
+// 20.2 us: 3 until the span is known, 10 for the tiles, 6 for the join.
 // Measured and slower: scores of 128 entries in one product (144 and 415 us: no second buffer), 16 warps for
 // the softmax (152, 424), next scores into registers during the exponentials (149), a part of the
 // exponentials as a polynomial (no gain), one warp for all matrix instructions (158).
@@ -58,7 +59,12 @@ constexpr int kTile = 64;        // cache entries of a tile
 // token on 8000 entries 20.8, 20.2, 20.0, 19.9, 19.9 us, 32 trees 136, 134, 131, 131, 133, prompts 384, 382, 376, 379, 380.
 constexpr int kOverhead = 6;
 constexpr int kGoRing = 16;      // more than the value tiles that their ring can hold
-constexpr int kFewRows = 32;     // a block of no more rows is copied row by row
+// A block of no more rows is copied row by row and the rest of its tile stays zeros; a box brings the rows of other
+// tokens, whose products nobody asks for but which draw power.  On long caches that lowers the clock: 128 sequences of
+// one token on 5000 entries 421 us, by boxes 448; of two tokens (8 rows) 467 and 505; 64 of four on 8000 entries 381 and 400.
+// On short ones a box saves the copy's latency: 64 of one token on 700 entries 73.1 and 72.1.  From 36 rows on
+// boxes are no slower on either (12 tokens: 70.3 us against 70.8 row by row).
+constexpr int kFewRows = 32;
 // log2 units the maximum may rise before the output is rescaled, and by which the reference lies below it
 template <typename T>
 constexpr float kLazy = T::kNegInfElem == 0xff80u ? 8.0f : 4.0f;
