@@ -42,8 +42,8 @@ typedef enum {
   GTO_ERR_CUDA = 4,        /* a CUDA runtime call failed                                 */
   GTO_ERR_NONFINITE = 5,   /* device status: a row's log-sum-exp was not finite          */
   GTO_ERR_TIMEOUT = 6,     /* device status: a wait inside gto_tree_attention or gto_verify_tree
-                              ran out; the outputs of that attention are unspecified, the
-                              sequences of that verification have accept_len -1            */
+                              ran out; the outputs of that attention are unspecified, a
+                              sequence that could not be verified has accept_len -1        */
   GTO_ERR_TOO_LARGE = 7,   /* gto_build_tree_noalloc: batch exceeds the fixed scratch    */
   GTO_ERR_BAD_INDEX = 8    /* device status: an index in a caller's table (d2t, a tree's
                               rows, tokens or parents, a path's rows, a page table, the

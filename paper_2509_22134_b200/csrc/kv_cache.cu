@@ -26,9 +26,9 @@ __device__ __forceinline__ void turn(double position, double inv_freq, float& c,
   sincospif(2.0f * f, &s, &c);
 }
 
-// One CTA per token, and one that looks at all sequences for those that contradict themselves.  A group of `lanes` lanes (a power of two, at least half the 16-byte vectors
-// of a head) takes one head at a time; a lane holds the two vectors whose elements rotate into
-// one another.
+// One CTA per token, and one that looks at all sequences for those that contradict themselves.  A group
+// of `lanes` lanes (a power of two, at least half the 16-byte vectors of a head) takes one head at a
+// time; a lane holds the two vectors whose elements rotate into one another.
 template <typename T, bool kInterleaved>
 __global__ void __launch_bounds__(kAppendThreads) kv_append_kernel(AppendArgs a, int lanes) {
   constexpr int E = T::kPerVec;

@@ -28,7 +28,8 @@
 // output.  bf16 has fp32's exponents.  fp16 has normal numbers from 2^-14 to 2^16 only: its reference lies
 // kRaise below the maximum, weights go up to 2^(kRaise + kLazy) = 2^15, and those down to 2^-25 of the
 // row's largest keep the half step (a long flat tail behind one large score is made of such weights);
-// what is below 2^-36 of it is lost.
+// what is below 2^-36 of it is lost.  Scores of 2^20 and more, where fp32 knows the exponent to a tenth only,
+// have their reference at the maximum: the weight of a rounding more must not pass 2^16.
 //
 // What bounds it (32 query heads, 8 key heads of 128; B200 at 1.7 to 1.97 GHz).  Single tokens: the copies;
 // 128 sequences of 1500 to 6000 entries take 340 to 370 us by the board, 5.4 to 5.8 TB/s (83 to 90 % of the
@@ -886,7 +887,8 @@ __global__ void __launch_bounds__(kThreads, 1)
             mask(tile);
             if (!ok) break;
           }
-          const float top = fmaxf(max_of(x[0]), max_of(x[1])) * sl - kRaise<T>;  // the reference of these scores
+          float top = fmaxf(max_of(x[0]), max_of(x[1])) * sl;  // to be the reference of these scores
+          if (kRaise<T> != 0.f) top -= fabsf(top) < 0x1p20f ? kRaise<T> : 0.f;
           if (j == j0) {
             m = top;
           } else {

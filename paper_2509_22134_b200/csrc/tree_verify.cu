@@ -711,8 +711,9 @@ cudaError_t verify_as(const VerifyArgs& a, cudaStream_t stream) {
 template <typename T>
 cudaError_t verify_as(const VerifyArgs& a, int sms, cudaStream_t stream) {
   // Two CTAs an SM may have 128 registers a thread: one tree of 32 000 ids took 13.2 us against 14.1 with
-  // 64.  Where the sequences do not fit the device so, four, with 64 registers, of which 80 bytes a thread spill: 128 trees of 128 256 ids took 84 us against
-  // 97 at three an SM, and 91 in clusters of four CTAs (all with the cluster's barrier for the exchange).
+  // 64.  Where the sequences do not fit the device so, four, with 64 registers (80 bytes a thread spill): 128
+  // trees of 128 256 ids took 84 us against 97 at three an SM, and 91 in clusters of four CTAs (all with the
+  // cluster's barrier for the exchange).
   const bool few = static_cast<int64_t>(a.S) * kCluster <= 2ll * sms;
   return few ? verify_as<T, 2>(a, stream) : verify_as<T, 4>(a, stream);
 }

@@ -94,3 +94,38 @@ def test_a_value_that_is_not_finite_spoils_no_lse_and_no_row_that_does_not_see_i
     blind = ~sees[:c.n]
     assert np.all(np.abs(got[blind] - want[:c.n][blind]) <= spread[:c.n][blind] * (dc.HALF_STEP[dtype] * 2 + 1e-3))
     assert not np.isfinite(got[sees[:c.n]]).any()
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("low", [23265282, 9000000, 726815, 1000])
+def test_scores_whose_exponents_fp32_knows_roughly_give_finite_weights(gto, low, dtype):
+    """Scores of `low` and a little more in later tiles, where fp32 numbers are up to 4 apart: the weight of an exponent
+    rounded up, relative to a reference below the maximum, could pass what fp16 holds.  All values are 1.5, so that the output
+    is 1.5 whatever the weights are, if they are finite: each is rounded (half a step), their sum is not, and the result once.
+    A score is unit a + b, all of them numbers of the type: exact in fp32."""
+    S, n, dh = 300, 500, 64
+    bits = 2 ** 11 if dtype == "f16" else 2 ** 8
+    k = torch.zeros((-(-n // 16), 16, 1, dh), dtype=torch.float64)
+    flat = k.view(-1, dh)
+    unit = 512 if low > 2 ** 24 else 256
+    a = low // unit
+    a -= a % max(1, 2 ** max(0, int(a).bit_length() - int(bits).bit_length() + 1))      # (a number that the type holds)
+    b = min(low - unit * a, 200)
+    for tile, more in enumerate([0, 2, 2, 6, 4, 2, 2]):
+        flat[tile * 64 + 7, 0] = a
+        flat[tile * 64 + 7, 1] = b + more
+    k, v = k.to(dc.TORCH[dtype]), torch.full_like(k, 1.5).to(dc.TORCH[dtype])
+    assert k[0, 7, 0, 0] == a
+    q = torch.zeros((S, 1, dh), dtype=dc.TORCH[dtype], device=DEV)
+    q[:, :, 0], q[:, :, 1] = unit, 1
+    batch = dict(q_start=torch.arange(S + 1, dtype=torch.int32, device=DEV), kv_len=torch.full((S,), n, dtype=torch.int32, device=DEV),
+                 page_table=torch.arange(k.shape[0], dtype=torch.int32, device=DEV).repeat(S, 1))
+    cfg = gto.make_decode_config(S=S, T=S, n_q_heads=1, n_kv_heads=1, head_dim=dh, page_size=16, n_pages=k.shape[0],
+                                 max_pages=k.shape[0], dtype=dtype, softmax_scale=1.0)
+    ctx = gto.gto_decode_create(cfg, 0)
+    out, lse = torch.zeros_like(q), torch.zeros((S, 1), device=DEV)
+    gto.gto_tree_attention(ctx, batch, q, k.to(DEV), v.to(DEV), out, lse=lse)
+    assert gto.gto_decode_status(ctx) == 0
+    assert torch.all((out.double() - 1.5).abs() <= 1.5 * (2 * dc.HALF_STEP[dtype] + 2.0 ** -20))
+    x = torch.from_numpy(float(unit * a + b) + np.array([0, 2, 2, 6, 4, 2, 2.0]))
+    assert torch.all((lse.double() - torch.logsumexp(x, 0)).abs() <= 2.0 ** -22 * x[0] + 2.0 ** -18)
