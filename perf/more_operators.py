@@ -228,7 +228,8 @@ def prepare(case, seed):
         else:
             hkv = case.get("hkv", 8)
             cfg = gto.make_decode_config(S=case["S"], T=case["S"], n_q_heads=hkv, n_kv_heads=hkv, head_dim=case.get("dh", 128),
-                                         page_size=case["page"], dtype=case.get("dtype", "bf16"), **s["size"])
+                                         page_size=case["page"], dtype=case.get("dtype", "bf16"),
+                                         flags=gto.GTO_DECODE_PAGES, **s["size"])
         # the library's context, as a program keeps it for as long as it decodes (it frees itself)
         s["ctx"] = gto.gto_decode_create(cfg, torch.cuda.current_device())
     return s
