@@ -48,7 +48,9 @@ typedef enum {
   GTO_ERR_BAD_INDEX = 8    /* device status: an index in a caller's table (d2t, a tree's
                               rows, tokens or parents, a path's rows, a page table, the
                               lengths of a batch) was out of range; the
-                              entry was skipped, results that depend on it are unspecified  */
+                              entry was skipped, results that depend on it are unspecified  */,
+  GTO_ERR_NO_PAGES = 9     /* device status: gto_pages_resize found too few free pages; the
+                              sequences that it could not serve are as they were            */
 } gto_status;
 
 typedef enum { GTO_F32 = 0, GTO_BF16 = 1, GTO_F16 = 2 } gto_dtype;
@@ -321,6 +323,8 @@ typedef struct gto_decode_ctx gto_decode_ctx;
 
 enum {
   GTO_DECODE_ROPE_INTERLEAVED = 1u, /* rotate the pairs (2i, 2i+1) instead of (i, i + rope_dims/2) */
+  GTO_DECODE_PAGES = 4u, /* the context serves gto_pages_fork, _resize and _compact: 4 (S max_pages + 3 n_pages)
+                            + 32 S bytes more of workspace                                     */
   GTO_DECODE_CONTEXT_ROWS = 2u /* gto_verify_tree reads target rows in the layout of
                                   gto_tree_reward, [S, R, V_target] with R = 1 + (D-1)k, through
                                   node_depth and node_slot; default: [S, 1+g, V_target], row 0
@@ -453,6 +457,78 @@ gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, cons
  * negative or above D, is reported and skipped. */
 gto_status gto_kv_commit(gto_decode_ctx* ctx, const gto_batch* batch, const gto_verdict* verdict,
                          const gto_kv_cache* cache, int32_t* kv_len_out, void* stream);
+
+/* Settings of N sequences, each with its own: what of softmax(z / temperature) a token may be drawn from.
+ * With w_i = exp((z_i - max z) / temperature) (weights below 2^-1000 are 0) and the tokens in the order (z
+ * descending, id ascending), a token of logit -inf never stays;
+ *   top_k > 0:     of the others the first top_k stay (<= 0: all);
+ *   top_p < 1:     of those the shortest run from the first on whose weights sum to top_p times the sum of all
+ *                  of them, one token at least (>= 1: all);
+ *   min_p > 0:     of those the ones with w_i >= min_p (min_p is clamped to [0, 1]).
+ * temperature 0: the arg-max alone (lowest id on ties).  temperature: [N]; the others [N] or NULL (no such limit). */
+typedef struct {
+  const float* temperature;
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+} gto_limits;
+
+/* Draws a token for each of N sequences (N <= S of the context): token[i] = the smallest id v of those that stay with
+ * sum_{w <= v} p(w) > u[i], p being the distribution over what stays of row i of the logits, or of row rows[i]
+ * (several sequences may draw from one row).  logits: [n_rows, V_target], row r at r * row_stride (elements, a multiple
+ * of 16 bytes).  u: [N] fp32, given by the caller, in [0, 1) (clamped to it).  logp ([N] or NULL): log p(token); 0 at
+ * temperature 0.  n_kept ([N] or NULL): how many tokens stay.  The decisions are those of fp64 sums.
+ * A sequence whose row holds NaN or +inf, or nothing but -inf, whose temperature is negative or not finite, or whose
+ * top_p or min_p is NaN, is reported (GTO_ERR_NONFINITE), one whose rows[i] names no row too (GTO_ERR_BAD_INDEX); it
+ * gets token -1, logp 0 and n_kept 0.  The outputs overlap neither one another nor what the call reads. */
+gto_status gto_sample_tokens(gto_decode_ctx* ctx, const void* logits, int64_t row_stride, int32_t n_rows,
+                             const int32_t* rows, int32_t N, const gto_limits* limits, const float* u,
+                             int32_t* token, float* logp, int32_t* n_kept, void* stream);
+
+/* gto_verify_tree with limits: p is the distribution over what stays of a context's row, and a drafted token that
+ * does not stay is never accepted.  The accepted tokens and the last one together follow the target's limited
+ * distribution, as gto_sample_tokens would draw them one by one. */
+gto_status gto_verify_tree_limited(gto_decode_ctx* ctx, const gto_draft_tree* tree, const void* target,
+                                   const int32_t* d2t, const gto_limits* limits, const float* u_node,
+                                   const float* u_bonus, const gto_verdict* out, void* stream);
+
+/* Who holds which pages of the cache.  Device arrays, changed by gto_pages_fork and gto_pages_resize; page_table and
+ * kv_len are those of a gto_batch.  A page that no sequence holds is free (ref_count 0): a pool begins with held,
+ * kv_len and ref_count 0. */
+typedef struct {
+  int32_t S;
+  int32_t* page_table;  /* [S, max_pages]; -1 behind the first held[s]                       */
+  int32_t* kv_len;      /* [S] entries, at most held[s] * page_size                          */
+  int32_t* held;        /* [S] pages, slots 0 .. held[s]-1 of the row                        */
+  int32_t* ref_count;   /* [n_pages] in how many held slots the page is named                */
+} gto_page_pool;
+
+/* Sequence s becomes a copy of sequence parent[s]: the same kv_len, and the same pages, shared (those with entries; pages
+ * that the parent holds beyond them are not).  What s held is given back.  parent[s] = s: s stays as it is; -1: it
+ * becomes empty.  All sequences are read as they were before the call, so any mapping will do (beams that change places).
+ * No cache entry is copied: gto_pages_resize does that for a page that is about to be written.  A sequence whose parent
+ * is none, or whose or whose parent's numbers contradict one another, is reported (GTO_ERR_BAD_INDEX) and stays as it is.
+ * parent: [S], overlaps none of the pool's arrays. */
+gto_status gto_pages_fork(gto_decode_ctx* ctx, const gto_page_pool* pool, const int32_t* parent, void* stream);
+
+/* Room for want[s] entries in every sequence with want[s] >= 0 (a negative one stays as it is): it then holds
+ * ceil(want[s] / page_size) pages, and kv_len[s] is at most want[s].  Pages beyond are given back (want[s] = 0: all).
+ * Where want[s] > kv_len[s], entries will be written from kv_len[s] on: slots from there on whose page another sequence
+ * holds too get a page of their own, and the first of them the entries below kv_len[s], in all layers (every sequence of the
+ * call that shares the page gets a copy; the old page is free if nobody kept it).  New pages are the lowest that were free
+ * before the call, in the order of the sequences; what the call gives back can be had by the next one.  A sequence for which
+ * too few are left stays as it is, and so do those behind it that need pages (GTO_ERR_NO_PAGES).  A sequence whose numbers contradict one
+ * another or whose want is above max_pages * page_size is reported (GTO_ERR_BAD_INDEX) and stays as it is.
+ * want: [S], overlaps none of the pool's arrays. */
+gto_status gto_pages_resize(gto_decode_ctx* ctx, const gto_page_pool* pool, const int32_t* want,
+                            const gto_kv_cache* cache, void* stream);
+
+/* Moves the pages in use to the front of the cache, in all layers: with *n_used of them, the i-th used page of those from
+ * n_used on goes to the i-th free place below n_used.  table_out [S, max_pages] and ref_out [n_pages] receive the pool's table
+ * and counts afterwards; the pool itself stays as it is, and valid, until a free page is written: copy them over the
+ * pool's arrays to go on with the new places.  The outputs overlap neither one another nor the pool's arrays. */
+gto_status gto_pages_compact(gto_decode_ctx* ctx, const gto_page_pool* pool, const gto_kv_cache* cache,
+                             int32_t* table_out, int32_t* ref_out, int32_t* n_used, void* stream);
 
 /* As gto_device_status and gto_launch_count, for a decoding context. */
 gto_status gto_decode_status(gto_decode_ctx* ctx, void* stream, int32_t* host_code);

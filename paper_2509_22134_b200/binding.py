@@ -114,7 +114,7 @@ for _f in ("gto_create", "gto_destroy", "gto_build_tree", "gto_tree_reward",
     getattr(_lib, _f).restype = ctypes.c_int
 
 
-GTO_DECODE_ROPE_INTERLEAVED, GTO_DECODE_CONTEXT_ROWS = 1, 2
+GTO_DECODE_ROPE_INTERLEAVED, GTO_DECODE_CONTEXT_ROWS, GTO_DECODE_PAGES = 1, 2, 4
 
 
 class gto_decode_config(ctypes.Structure):
@@ -129,6 +129,14 @@ class gto_batch(ctypes.Structure):
     _fields_ = [("S", ctypes.c_int32), ("T", ctypes.c_int32)] + \
                [(n, ctypes.c_void_p) for n in
                 ("q_start", "kv_len", "page_table", "n_nodes", "node_mask", "node_depth")]
+
+
+class gto_limits(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_k", "top_p", "min_p")]
+
+
+class gto_page_pool(ctypes.Structure):
+    _fields_ = [("S", ctypes.c_int32)] + [(n, ctypes.c_void_p) for n in ("page_table", "kv_len", "held", "ref_count")]
 
 
 class gto_kv_cache(ctypes.Structure):
@@ -456,6 +464,51 @@ def gto_kv_commit(ctx: DecodeCtx, batch: dict, verdict: dict, k_cache, v_cache, 
         raise GtoError(code, "gto_kv_commit")
 
 
+def gto_sample_tokens(ctx: DecodeCtx, logits, limits: dict, u, token, logp=None, n_kept=None, rows=None, stream=None):
+    """logits: [n_rows, V_target], rows dense, any stride of 16 bytes; limits: dict of temperature [N] and, optionally,
+    top_k [N] (int32), top_p [N] and min_p [N]; u [N]; token [N] (int32), logp [N], n_kept [N] (int32): outputs; rows [N]
+    (int32): the row that each draws from (default: its own)."""
+    code = _native.sample_tokens(ctx.native, logits, limits, u, token, logp, n_kept, rows, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_sample_tokens")
+
+
+def gto_verify_tree_limited(ctx: DecodeCtx, tree: dict, target, d2t, limits: dict, u_node, u_bonus, verdict: dict, stream=None):
+    """As gto_verify_tree, with the limits of gto_sample_tokens."""
+    code = _native.verify_tree_limited(ctx.native, tree, target, d2t, limits, u_node, u_bonus, verdict, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_verify_tree_limited")
+
+
+def alloc_page_pool(cfg: gto_decode_config, device, S=None) -> dict:
+    """An empty pool: nobody holds a page."""
+    S = cfg.S if S is None else S
+    i32 = dict(dtype=torch.int32, device=device)
+    return {"page_table": torch.full((S, cfg.max_pages), -1, **i32), "kv_len": torch.zeros(S, **i32),
+            "held": torch.zeros(S, **i32), "ref_count": torch.zeros(cfg.n_pages, **i32)}
+
+
+def gto_pages_fork(ctx: DecodeCtx, pool: dict, parent, stream=None):
+    """pool: dict of page_table [S, max_pages], kv_len [S], held [S] and ref_count [n_pages] (int32); parent [S] (int32)."""
+    code = _native.pages_fork(ctx.native, pool, parent, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_pages_fork")
+
+
+def gto_pages_resize(ctx: DecodeCtx, pool: dict, want, k_cache, v_cache, stream=None):
+    """want [S] (int32); k_cache, v_cache: [n_pages, ...] of one layer or [n_layers, n_pages, ...] of all."""
+    code = _native.pages_resize(ctx.native, pool, want, k_cache, v_cache, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_pages_resize")
+
+
+def gto_pages_compact(ctx: DecodeCtx, pool: dict, k_cache, v_cache, table_out, ref_out, n_used, stream=None):
+    """table_out [S, max_pages], ref_out [n_pages], n_used [1] (int32): the pool's table and counts afterwards, the pages in use."""
+    code = _native.pages_compact(ctx.native, pool, k_cache, v_cache, table_out, ref_out, n_used, _stream_of(ctx, stream))
+    if code:
+        raise GtoError(code, "gto_pages_compact")
+
+
 def gto_decode_status(ctx: DecodeCtx, stream=None) -> int:
     code = ctypes.c_int32(0)
     _check(_lib.gto_decode_status(ctx.handle, _stream_of(ctx, stream), ctypes.byref(code)), "gto_decode_status")
@@ -470,4 +523,5 @@ EXPORTS = ["gto_create", "gto_destroy", "gto_build_tree", "gto_tree_reward",
            "gto_group_surrogate_grad", "gto_device_status", "gto_launch_count", "gto_status_string",
            "gto_kernel_timing", "gto_kernel_times", "gto_build_tree_noalloc", "gto_token_loss", "gto_sample_groups", "gto_tree_reward_host",
            "gto_token_loss_accumulate", "gto_decode_create", "gto_decode_destroy", "gto_kv_append",
-           "gto_tree_attention", "gto_verify_tree", "gto_kv_commit", "gto_decode_status", "gto_decode_launch_count"]
+           "gto_tree_attention", "gto_verify_tree", "gto_kv_commit", "gto_sample_tokens",
+           "gto_verify_tree_limited", "gto_pages_fork", "gto_pages_resize", "gto_pages_compact", "gto_decode_status", "gto_decode_launch_count"]

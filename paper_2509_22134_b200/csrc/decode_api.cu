@@ -15,6 +15,7 @@ struct gto_decode_ctx {
   char* ws;          // one allocation
   int32_t* status;
   char* attn_ws;     // parts of blocks that were cut, null where the tensor-core kernel does not serve
+  char* pages_ws;    // plans of the page calls, null without GTO_DECODE_PAGES
   int64_t launches;
 };
 
@@ -118,6 +119,77 @@ gto_status cache_args(const gto_decode_ctx* ctx, const gto_kv_cache* in, gto::Ca
   return GTO_OK;
 }
 
+// What both forms of the verification check; limits: further arrays of S words that they read.
+gto_status verify_args(const gto_decode_config& c, const gto_draft_tree* tree, const void* target, const int32_t* d2t,
+                       const float* temperature, const float* u_node, const float* u_bonus, const gto_verdict* out,
+                       std::initializer_list<const void*> limits) {
+  if (!table(target, 16) || !table(temperature, 4) || !table(u_bonus, 4) || !table(out->accept_len, 4) ||
+      !table(out->path_node, 4) || !table(out->token, 4) || (d2t && !aligned(d2t, 4)))
+    return GTO_ERR_INVALID_ARG;
+  if (c.g > 0 && (!table(tree->node_token, 4) || !table(tree->node_parent, 4) || !table(u_node, 4)))
+    return GTO_ERR_INVALID_ARG;
+  if (tree->n_nodes && !aligned(tree->n_nodes, 4)) return GTO_ERR_INVALID_ARG;
+  if (!d2t && c.V_draft != c.V_target) return GTO_ERR_INVALID_ARG;
+  const bool ctx_rows = (c.flags & GTO_DECODE_CONTEXT_ROWS) != 0;
+  if (ctx_rows && c.g > 0 && (!table(tree->node_depth, 4) || !table(tree->node_slot, 4)))
+    return GTO_ERR_INVALID_ARG;
+  const size_t S = tree->S, word = sizeof(int32_t), nodes = word * S * c.g;
+  const size_t target_rows = ctx_rows ? 1 + static_cast<size_t>(c.D - 1) * c.k : 1 + static_cast<size_t>(c.g);
+  const Array outs[3] = {{out->accept_len, word * S}, {out->path_node, word * S * c.D}, {out->token, word * S * (c.D + 1)}};
+  for (int i = 0; i < 3; ++i)
+    if (over_any(outs[i], {outs[(i + 1) % 3], {tree->node_token, nodes}, {tree->node_parent, nodes},
+                           {ctx_rows ? tree->node_depth : nullptr, nodes}, {ctx_rows ? tree->node_slot : nullptr, nodes},
+                           {tree->n_nodes, word * S}, {target, S * target_rows * c.V_target * gto::elem_bytes(c.logit_dtype)},
+                           {d2t, word * c.V_draft}, {temperature, word * S}, {u_node, nodes}, {u_bonus, word * S}}))
+      return GTO_ERR_INVALID_ARG;
+  for (const void* x : limits)
+    for (int i = 0; i < 3; ++i)
+      if (over_any(outs[i], {{x, word * S}})) return GTO_ERR_INVALID_ARG;
+  return GTO_OK;
+}
+
+gto_status limit_args(const gto_limits* in, gto::LimitedArgs* a) {
+  if (!in || !table(in->temperature, 4) || (in->top_k && !aligned(in->top_k, 4)) || (in->top_p && !aligned(in->top_p, 4)) ||
+      (in->min_p && !aligned(in->min_p, 4)))
+    return GTO_ERR_INVALID_ARG;
+  a->temperature = in->temperature;
+  a->top_k = in->top_k;
+  a->top_p = in->top_p;
+  a->min_p = in->min_p;
+  return GTO_OK;
+}
+
+gto_status pool_args(const gto_decode_ctx* ctx, const gto_page_pool* in, gto::PoolArgs* out) {
+  const gto_decode_config& c = ctx->cfg;
+  if (!in || in->S < 0 || in->S > c.S || !ctx->pages_ws) return GTO_ERR_INVALID_ARG;
+  out->S = in->S;
+  if (in->S == 0) return GTO_OK;
+  if (!table(in->page_table, 4) || !table(in->kv_len, 4) || !table(in->held, 4) || !table(in->ref_count, 4))
+    return GTO_ERR_INVALID_ARG;
+  const size_t word = sizeof(int32_t), S = in->S;
+  const Array all[4] = {{in->page_table, word * S * c.max_pages}, {in->kv_len, word * S}, {in->held, word * S},
+                        {in->ref_count, word * c.n_pages}};
+  for (int i = 0; i < 3; ++i)
+    for (int j = i + 1; j < 4; ++j)
+      if (over_any(all[i], {all[j]})) return GTO_ERR_INVALID_ARG;
+  out->page_size = c.page_size;
+  out->n_pages = c.n_pages;
+  out->max_pages = c.max_pages;
+  out->page_table = in->page_table;
+  out->kv_len = in->kv_len;
+  out->held = in->held;
+  out->ref_count = in->ref_count;
+  out->status = ctx->status;
+  return GTO_OK;
+}
+
+// Whether an array lies over one of the pool's.
+bool over_pool(const gto_decode_ctx* ctx, const gto_page_pool* p, Array x) {
+  const size_t word = sizeof(int32_t), S = p->S;
+  return over_any(x, {{p->page_table, word * S * ctx->cfg.max_pages}, {p->kv_len, word * S}, {p->held, word * S},
+                      {p->ref_count, word * ctx->cfg.n_pages}});
+}
+
 }  // namespace
 
 extern "C" {
@@ -127,9 +199,9 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
   *out = nullptr;
   if (c->S <= 0 || c->T < 0 || c->g < 0 || c->D < 1 || c->n_kv_heads < 0 || c->V_target < 0)
     return GTO_ERR_INVALID_ARG;
-  if (c->flags & ~static_cast<uint32_t>(GTO_DECODE_ROPE_INTERLEAVED | GTO_DECODE_CONTEXT_ROWS))
+  if (c->flags & ~static_cast<uint32_t>(GTO_DECODE_ROPE_INTERLEAVED | GTO_DECODE_CONTEXT_ROWS | GTO_DECODE_PAGES))
     return GTO_ERR_INVALID_ARG;
-  if (c->n_kv_heads == 0 && c->V_target == 0) return GTO_ERR_INVALID_ARG;
+  if (c->n_kv_heads == 0 && (c->V_target == 0 || (c->flags & GTO_DECODE_PAGES))) return GTO_ERR_INVALID_ARG;
   if (c->g > gto::kMaxNodes || c->D > gto::kMaxDepth) return GTO_ERR_UNSUPPORTED;
   if (c->n_kv_heads > 0) {
     if (c->n_q_heads <= 0 || c->n_q_heads % c->n_kv_heads || c->head_dim <= 0 || c->page_size <= 0 ||
@@ -142,6 +214,8 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
         c->rope_dims % 16 || c->n_kv_heads > 65535)
       return GTO_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(c->max_pages) * c->page_size > (1ll << 31) - 256) return GTO_ERR_UNSUPPORTED;
+    // the page calls have a copy of the table
+    if ((c->flags & GTO_DECODE_PAGES) && static_cast<int64_t>(c->S) * c->max_pages > (1ll << 33)) return GTO_ERR_UNSUPPORTED;
     // work units of a call are counted in 32 bits
     if (static_cast<int64_t>(c->T) * c->n_q_heads + c->S >= (1ll << 30)) return GTO_ERR_UNSUPPORTED;
   }
@@ -170,13 +244,16 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
     return GTO_ERR_CUDA;
   }
   const bool tc = c->n_kv_heads > 0 && gto::attention_tc_serves(*c);
-  if (cudaMalloc(&ctx->ws, 256 + (tc ? gto::attention_tc_workspace(*c, ctx->sms) : 0)) != cudaSuccess) {
+  const size_t attn = tc ? (gto::attention_tc_workspace(*c, ctx->sms) + 255) / 256 * 256 : 0;
+  const size_t pages = (c->flags & GTO_DECODE_PAGES) ? gto::pages_workspace(*c) : 0;
+  if (cudaMalloc(&ctx->ws, 256 + attn + pages) != cudaSuccess) {
     cudaGetLastError();
     delete ctx;
     return GTO_ERR_WORKSPACE;
   }
   ctx->status = reinterpret_cast<int32_t*>(ctx->ws);
   ctx->attn_ws = tc ? ctx->ws + 256 : nullptr;
+  ctx->pages_ws = (c->flags & GTO_DECODE_PAGES) ? ctx->ws + 256 + attn : nullptr;
   // (waited for: the first call may come on a stream that the default one does not order)
   if (cudaMemset(ctx->ws, 0, 256) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
     cudaGetLastError();
@@ -293,25 +370,9 @@ gto_status gto_verify_tree(gto_decode_ctx* ctx, const gto_draft_tree* tree, cons
   const gto_decode_config& c = ctx->cfg;
   if (!tree || !out || c.V_target == 0 || tree->S < 0 || tree->S > c.S) return GTO_ERR_INVALID_ARG;
   if (tree->S == 0) return GTO_OK;
-  if (!table(target, 16) || !table(temperature, 4) || !table(u_bonus, 4) || !table(out->accept_len, 4) ||
-      !table(out->path_node, 4) || !table(out->token, 4) || (d2t && !aligned(d2t, 4)))
-    return GTO_ERR_INVALID_ARG;
-  if (c.g > 0 && (!table(tree->node_token, 4) || !table(tree->node_parent, 4) || !table(u_node, 4)))
-    return GTO_ERR_INVALID_ARG;
-  if (tree->n_nodes && !aligned(tree->n_nodes, 4)) return GTO_ERR_INVALID_ARG;
-  if (!d2t && c.V_draft != c.V_target) return GTO_ERR_INVALID_ARG;
+  const gto_status st = verify_args(c, tree, target, d2t, temperature, u_node, u_bonus, out, {});
+  if (st != GTO_OK) return st;
   const bool ctx_rows = (c.flags & GTO_DECODE_CONTEXT_ROWS) != 0;
-  if (ctx_rows && c.g > 0 && (!table(tree->node_depth, 4) || !table(tree->node_slot, 4)))
-    return GTO_ERR_INVALID_ARG;
-  const size_t S = tree->S, word = sizeof(int32_t), nodes = word * S * c.g;
-  const size_t target_rows = ctx_rows ? 1 + static_cast<size_t>(c.D - 1) * c.k : 1 + static_cast<size_t>(c.g);
-  const Array outs[3] = {{out->accept_len, word * S}, {out->path_node, word * S * c.D}, {out->token, word * S * (c.D + 1)}};
-  for (int i = 0; i < 3; ++i)
-    if (over_any(outs[i], {outs[(i + 1) % 3], {tree->node_token, nodes}, {tree->node_parent, nodes},
-                           {ctx_rows ? tree->node_depth : nullptr, nodes}, {ctx_rows ? tree->node_slot : nullptr, nodes},
-                           {tree->n_nodes, word * S}, {target, S * target_rows * c.V_target * gto::elem_bytes(c.logit_dtype)},
-                           {d2t, word * c.V_draft}, {temperature, word * S}, {u_node, nodes}, {u_bonus, word * S}}))
-      return GTO_ERR_INVALID_ARG;
   gto::VerifyArgs a{};
   a.S = tree->S;
   a.g = c.g;
@@ -371,6 +432,146 @@ gto_status gto_kv_commit(gto_decode_ctx* ctx, const gto_batch* batch, const gto_
   return GTO_OK;
 }
 
+gto_status gto_sample_tokens(gto_decode_ctx* ctx, const void* logits, int64_t row_stride, int32_t n_rows,
+                             const int32_t* rows, int32_t N, const gto_limits* limits, const float* u, int32_t* token,
+                             float* logp, int32_t* n_kept, void* stream) {
+  if (!ctx) return GTO_ERR_INVALID_ARG;
+  CallRange range("gto_sample_tokens");
+  const gto_decode_config& c = ctx->cfg;
+  if (c.V_target == 0 || N < 0 || N > c.S || n_rows < 0 || (!rows && n_rows < N)) return GTO_ERR_INVALID_ARG;
+  if (N == 0) return GTO_OK;
+  const int64_t e = gto::elem_bytes(c.logit_dtype), row = c.V_target * e;
+  if (row_stride < c.V_target || row_stride >= (1ll << 40) || (row_stride * e) % 16 || (n_rows > 0 && !table(logits, 16)) ||
+      (rows && !aligned(rows, 4)) || !table(u, 4) || !table(token, 4) || (logp && !aligned(logp, 4)) ||
+      (n_kept && !aligned(n_kept, 4)))
+    return GTO_ERR_INVALID_ARG;
+  gto::LimitedArgs a{};
+  const gto_status st = limit_args(limits, &a);
+  if (st != GTO_OK) return st;
+  const size_t size = sizeof(int32_t) * N;
+  const Array outs[3] = {{token, size}, {logp, size}, {n_kept, size}};
+  for (int i = 0; i < 3; ++i)
+    if (outs[i].p && over_any(outs[i], {outs[(i + 1) % 3], {logits, span(n_rows, row_stride * e, row)}, {rows, size},
+                                        {a.temperature, size}, {a.top_k, size}, {a.top_p, size}, {a.min_p, size}, {u, size}}))
+      return GTO_ERR_INVALID_ARG;
+  a.N = N;
+  a.V = c.V_target;
+  a.dtype = c.logit_dtype;
+  a.logits = static_cast<const char*>(logits);
+  a.row_stride = row_stride * e;
+  a.u = u;
+  a.token = token;
+  a.status = ctx->status;
+  a.rows = rows;
+  a.n_rows = n_rows;
+  a.logp = logp;
+  a.n_kept = n_kept;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return GTO_ERR_CUDA;
+  if (gto::launch_limited(a, false, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess) return GTO_ERR_CUDA;
+  return GTO_OK;
+}
+
+gto_status gto_verify_tree_limited(gto_decode_ctx* ctx, const gto_draft_tree* tree, const void* target, const int32_t* d2t,
+                                   const gto_limits* limits, const float* u_node, const float* u_bonus,
+                                   const gto_verdict* out, void* stream) {
+  if (!ctx) return GTO_ERR_INVALID_ARG;
+  CallRange range("gto_verify_tree_limited");
+  const gto_decode_config& c = ctx->cfg;
+  if (!tree || !out || c.V_target == 0 || tree->S < 0 || tree->S > c.S) return GTO_ERR_INVALID_ARG;
+  if (tree->S == 0) return GTO_OK;
+  gto::LimitedArgs a{};
+  const gto_status st = limit_args(limits, &a);
+  if (st != GTO_OK) return st;
+  const gto_status sv = verify_args(c, tree, target, d2t, a.temperature, u_node, u_bonus, out, {a.top_k, a.top_p, a.min_p});
+  if (sv != GTO_OK) return sv;
+  const bool ctx_rows = (c.flags & GTO_DECODE_CONTEXT_ROWS) != 0;
+  a.N = tree->S;
+  a.V = c.V_target;
+  a.dtype = c.logit_dtype;
+  a.logits = static_cast<const char*>(target);
+  a.row_stride = static_cast<int64_t>(c.V_target) * gto::elem_bytes(c.logit_dtype);
+  a.u = u_bonus;
+  a.token = out->token;
+  a.status = ctx->status;
+  a.g = c.g;
+  a.D = c.D;
+  a.k = c.k;
+  a.V_draft = c.V_draft;
+  a.context_rows = ctx_rows;
+  a.rows_of_tree = ctx_rows ? 1 + (c.D - 1) * c.k : 1 + c.g;
+  a.node_token = tree->node_token;
+  a.node_parent = tree->node_parent;
+  a.node_depth = tree->node_depth;
+  a.node_slot = tree->node_slot;
+  a.n_nodes = tree->n_nodes;
+  a.d2t = d2t;
+  a.u_node = u_node;
+  a.accept_len = out->accept_len;
+  a.path_node = out->path_node;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return GTO_ERR_CUDA;
+  if (gto::launch_limited(a, true, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess) return GTO_ERR_CUDA;
+  return GTO_OK;
+}
+
+gto_status gto_pages_fork(gto_decode_ctx* ctx, const gto_page_pool* pool, const int32_t* parent, void* stream) {
+  if (!ctx) return GTO_ERR_INVALID_ARG;
+  CallRange range("gto_pages_fork");
+  gto::PoolArgs p{};
+  const gto_status st = pool_args(ctx, pool, &p);
+  if (st != GTO_OK) return st;
+  if (p.S == 0) return GTO_OK;
+  if (!table(parent, 4) || over_pool(ctx, pool, {parent, sizeof(int32_t) * p.S})) return GTO_ERR_INVALID_ARG;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return GTO_ERR_CUDA;
+  if (gto::launch_pages_fork(p, parent, ctx->pages_ws, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess)
+    return GTO_ERR_CUDA;
+  return GTO_OK;
+}
+
+gto_status gto_pages_resize(gto_decode_ctx* ctx, const gto_page_pool* pool, const int32_t* want, const gto_kv_cache* cache,
+                            void* stream) {
+  if (!ctx) return GTO_ERR_INVALID_ARG;
+  CallRange range("gto_pages_resize");
+  gto::PoolArgs p{};
+  gto::CacheArgs c{};
+  gto_status st = pool_args(ctx, pool, &p);
+  if (st == GTO_OK) st = cache_args(ctx, cache, &c);
+  if (st != GTO_OK) return st;
+  if (p.S == 0) return GTO_OK;
+  if (!table(want, 4) || over_pool(ctx, pool, {want, sizeof(int32_t) * p.S})) return GTO_ERR_INVALID_ARG;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return GTO_ERR_CUDA;
+  if (gto::launch_pages_resize(p, want, c, ctx->pages_ws, ctx->sms, static_cast<cudaStream_t>(stream), &ctx->launches) !=
+      cudaSuccess)
+    return GTO_ERR_CUDA;
+  return GTO_OK;
+}
+
+gto_status gto_pages_compact(gto_decode_ctx* ctx, const gto_page_pool* pool, const gto_kv_cache* cache, int32_t* table_out,
+                             int32_t* ref_out, int32_t* n_used, void* stream) {
+  if (!ctx) return GTO_ERR_INVALID_ARG;
+  CallRange range("gto_pages_compact");
+  gto::PoolArgs p{};
+  gto::CacheArgs c{};
+  gto_status st = pool_args(ctx, pool, &p);
+  if (st == GTO_OK) st = cache_args(ctx, cache, &c);
+  if (st != GTO_OK) return st;
+  if (p.S == 0) return GTO_OK;
+  if (!table(table_out, 4) || !table(ref_out, 4) || !table(n_used, 4)) return GTO_ERR_INVALID_ARG;
+  const size_t word = sizeof(int32_t);
+  const Array outs[3] = {{table_out, word * p.S * p.max_pages}, {ref_out, word * p.n_pages}, {n_used, word}};
+  for (int i = 0; i < 3; ++i)
+    if (over_pool(ctx, pool, outs[i]) || over_any(outs[i], {outs[(i + 1) % 3]})) return GTO_ERR_INVALID_ARG;
+  DeviceGuard guard(ctx->device);
+  if (!guard.ok) return GTO_ERR_CUDA;
+  if (gto::launch_pages_compact(p, c, table_out, ref_out, n_used, ctx->pages_ws, ctx->sms, static_cast<cudaStream_t>(stream),
+                                &ctx->launches) != cudaSuccess)
+    return GTO_ERR_CUDA;
+  return GTO_OK;
+}
+
 gto_status gto_decode_status(gto_decode_ctx* ctx, void* stream, int32_t* host_code) {
   if (!ctx || !host_code) return GTO_ERR_INVALID_ARG;
   DeviceGuard guard(ctx->device);
@@ -383,6 +584,7 @@ gto_status gto_decode_status(gto_decode_ctx* ctx, void* stream, int32_t* host_co
     return GTO_ERR_CUDA;
   *host_code = (word & gto::kStatusTimeout)     ? GTO_ERR_TIMEOUT
                : (word & gto::kStatusBadIndex)  ? GTO_ERR_BAD_INDEX
+               : (word & gto::kStatusNoPages)   ? GTO_ERR_NO_PAGES
                : (word & gto::kStatusNonFinite) ? GTO_ERR_NONFINITE
                                                 : GTO_OK;
   return GTO_OK;

@@ -238,34 +238,58 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+gto_draft_tree tree_of(const Ctx& c, PyObject* dict, int64_t S) {
+  static PyObject *node_token = key("node_token"), *node_parent = key("node_parent"), *node_depth = key("node_depth"),
+                  *node_slot = key("node_slot"), *n_nodes = key("n_nodes");
+  const int64_t g = c.cfg.g;
+  gto_draft_tree t{};
+  t.S = small(S, "temperature");
+  if (g == 0) return t;
+  if (!PyDict_Check(dict)) {
+    PyErr_SetString(PyExc_ValueError, "tree: expected a dict");
+    throw Raised{};
+  }
+  const auto node = [&](PyObject* name, const char* s) {
+    return static_cast<const int32_t*>(dense(c, need(dict, name), s, at::kInt, I2{S, g}));
+  };
+  t.node_token = node(node_token, "node_token");
+  t.node_parent = node(node_parent, "node_parent");
+  if (c.cfg.flags & GTO_DECODE_CONTEXT_ROWS) {
+    t.node_depth = node(node_depth, "node_depth");
+    t.node_slot = node(node_slot, "node_slot");
+  }
+  t.n_nodes = static_cast<const int32_t*>(maybe(c, get(dict, n_nodes), "n_nodes", at::kInt, I1{S}));
+  return t;
+}
+
+const void* target_of(const Ctx& c, PyObject* o, int64_t S) {
+  const int64_t R = (c.cfg.flags & GTO_DECODE_CONTEXT_ROWS) ? 1 + static_cast<int64_t>(c.cfg.D - 1) * c.cfg.k : 1 + c.cfg.g;
+  return dense(c, o, "target", c.logit, I3{S, R, c.cfg.V_target});
+}
+
+// Settings of N sequences; their number is that of the temperatures.
+int64_t limits_of(const Ctx& c, PyObject* dict, gto_limits* out) {
+  static PyObject *temperature = key("temperature"), *top_k = key("top_k"), *top_p = key("top_p"), *min_p = key("min_p");
+  if (!PyDict_Check(dict)) {
+    PyErr_SetString(PyExc_ValueError, "limits: expected a dict");
+    throw Raised{};
+  }
+  PyObject* t = need(dict, temperature);
+  const int64_t N = first_size(t, "temperature");
+  out->temperature = static_cast<const float*>(dense(c, t, "temperature", at::kFloat, I1{N}));
+  out->top_k = static_cast<const int32_t*>(maybe(c, get(dict, top_k), "top_k", at::kInt, I1{N}));
+  out->top_p = static_cast<const float*>(maybe(c, get(dict, top_p), "top_p", at::kFloat, I1{N}));
+  out->min_p = static_cast<const float*>(maybe(c, get(dict, min_p), "min_p", at::kFloat, I1{N}));
+  return N;
+}
+
 // (ctx, tree, target, d2t, temperature, u_node, u_bonus, verdict, stream)
 PyObject* verify_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
   return guarded(n, 9, [&]() -> long {
-    static PyObject *node_token = key("node_token"), *node_parent = key("node_parent"), *node_depth = key("node_depth"),
-                    *node_slot = key("node_slot"), *n_nodes = key("n_nodes");
     const Ctx& c = context(a[0]);
     const int64_t S = first_size(a[4], "temperature"), g = c.cfg.g;
-    const bool ctx_rows = (c.cfg.flags & GTO_DECODE_CONTEXT_ROWS) != 0;
-    gto_draft_tree t{};
-    t.S = small(S, "temperature");
-    if (g > 0) {
-      if (!PyDict_Check(a[1])) {
-        PyErr_SetString(PyExc_ValueError, "tree: expected a dict");
-        throw Raised{};
-      }
-      const auto node = [&](PyObject* name, const char* s) {
-        return static_cast<const int32_t*>(dense(c, need(a[1], name), s, at::kInt, I2{S, g}));
-      };
-      t.node_token = node(node_token, "node_token");
-      t.node_parent = node(node_parent, "node_parent");
-      if (ctx_rows) {
-        t.node_depth = node(node_depth, "node_depth");
-        t.node_slot = node(node_slot, "node_slot");
-      }
-      t.n_nodes = static_cast<const int32_t*>(maybe(c, get(a[1], n_nodes), "n_nodes", at::kInt, I1{S}));
-    }
-    const int64_t R = ctx_rows ? 1 + static_cast<int64_t>(c.cfg.D - 1) * c.cfg.k : 1 + g;
-    const void* target = dense(c, a[2], "target", c.logit, I3{S, R, c.cfg.V_target});
+    const gto_draft_tree t = tree_of(c, a[1], S);
+    const void* target = target_of(c, a[2], S);
     const void* d2t = maybe(c, a[3], "d2t", at::kInt, I1{c.cfg.V_draft});
     const void* temperature = dense(c, a[4], "temperature", at::kFloat, I1{S});
     const void* u_node = maybe(c, a[5], "u_node", at::kFloat, I2{S, g});
@@ -273,6 +297,95 @@ PyObject* verify_tree(PyObject*, PyObject* const* a, Py_ssize_t n) {
     const gto_verdict out = verdict_of(c, a[7], S);
     return gto_verify_tree(c.handle, &t, target, static_cast<const int32_t*>(d2t), static_cast<const float*>(temperature),
                            static_cast<const float*>(u_node), static_cast<const float*>(u_bonus), &out, stream_of(a[8]));
+  });
+}
+
+// (ctx, tree, target, d2t, limits, u_node, u_bonus, verdict, stream)
+PyObject* verify_tree_limited(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> long {
+    const Ctx& c = context(a[0]);
+    gto_limits limits{};
+    const int64_t S = limits_of(c, a[4], &limits), g = c.cfg.g;
+    const gto_draft_tree t = tree_of(c, a[1], S);
+    const void* target = target_of(c, a[2], S);
+    const void* d2t = maybe(c, a[3], "d2t", at::kInt, I1{c.cfg.V_draft});
+    const void* u_node = maybe(c, a[5], "u_node", at::kFloat, I2{S, g});
+    const void* u_bonus = dense(c, a[6], "u_bonus", at::kFloat, I1{S});
+    const gto_verdict out = verdict_of(c, a[7], S);
+    return gto_verify_tree_limited(c.handle, &t, target, static_cast<const int32_t*>(d2t), &limits,
+                                   static_cast<const float*>(u_node), static_cast<const float*>(u_bonus), &out, stream_of(a[8]));
+  });
+}
+
+// (ctx, logits, limits, u, token, logp, n_kept, rows, stream)
+PyObject* sample_tokens(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 9, [&]() -> long {
+    const Ctx& c = context(a[0]);
+    gto_limits limits{};
+    const int64_t N = limits_of(c, a[2], &limits), V = c.cfg.V_target;
+    const at::Tensor& z = tensor(a[1], "logits");
+    if (!here(c, z, c.logit) || z.dim() != 2 || z.size(1) != V || (z.size(0) > 0 && V > 1 && z.stride(1) != 1))
+      refuse(c, "logits", c.logit, "[rows, " + std::to_string(V) + "] with dense rows", z);
+    const void* u = dense(c, a[3], "u", at::kFloat, I1{N});
+    void* token = dense(c, a[4], "token", at::kInt, I1{N});
+    void* logp = maybe(c, a[5], "logp", at::kFloat, I1{N});
+    void* kept = maybe(c, a[6], "n_kept", at::kInt, I1{N});
+    const void* rows = maybe(c, a[7], "rows", at::kInt, I1{N});
+    if (a[7] == Py_None && z.size(0) != N) refuse(c, "logits", c.logit, "[" + std::to_string(N) + ", V] without rows", z);
+    return gto_sample_tokens(c.handle, z.data_ptr(), z.size(0) > 1 ? z.stride(0) : V, small(z.size(0), "logits"),
+                             static_cast<const int32_t*>(rows), small(N, "temperature"), &limits, static_cast<const float*>(u),
+                             static_cast<int32_t*>(token), static_cast<float*>(logp), static_cast<int32_t*>(kept), stream_of(a[8]));
+  });
+}
+
+gto_page_pool pool_of(const Ctx& c, PyObject* dict) {
+  static PyObject *page_table = key("page_table"), *kv_len = key("kv_len"), *held = key("held"), *ref_count = key("ref_count");
+  if (!PyDict_Check(dict)) {
+    PyErr_SetString(PyExc_ValueError, "pool: expected a dict");
+    throw Raised{};
+  }
+  const int64_t S = first_size(need(dict, kv_len), "kv_len");
+  gto_page_pool p{};
+  p.S = small(S, "kv_len");
+  p.page_table = static_cast<int32_t*>(dense(c, need(dict, page_table), "page_table", at::kInt, I2{S, c.cfg.max_pages}));
+  p.kv_len = static_cast<int32_t*>(dense(c, need(dict, kv_len), "kv_len", at::kInt, I1{S}));
+  p.held = static_cast<int32_t*>(dense(c, need(dict, held), "held", at::kInt, I1{S}));
+  p.ref_count = static_cast<int32_t*>(dense(c, need(dict, ref_count), "ref_count", at::kInt, I1{c.cfg.n_pages}));
+  return p;
+}
+
+// (ctx, pool, parent, stream)
+PyObject* pages_fork(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 4, [&]() -> long {
+    const Ctx& c = context(a[0]);
+    const gto_page_pool p = pool_of(c, a[1]);
+    const void* parent = dense(c, a[2], "parent", at::kInt, I1{p.S});
+    return gto_pages_fork(c.handle, &p, static_cast<const int32_t*>(parent), stream_of(a[3]));
+  });
+}
+
+// (ctx, pool, want, k_cache, v_cache, stream)
+PyObject* pages_resize(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 6, [&]() -> long {
+    const Ctx& c = context(a[0]);
+    const gto_page_pool p = pool_of(c, a[1]);
+    const void* want = dense(c, a[2], "want", at::kInt, I1{p.S});
+    const gto_kv_cache cache = cache_of(c, a[3], a[4], true);
+    return gto_pages_resize(c.handle, &p, static_cast<const int32_t*>(want), &cache, stream_of(a[5]));
+  });
+}
+
+// (ctx, pool, k_cache, v_cache, table_out, ref_out, n_used, stream)
+PyObject* pages_compact(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return guarded(n, 8, [&]() -> long {
+    const Ctx& c = context(a[0]);
+    const gto_page_pool p = pool_of(c, a[1]);
+    const gto_kv_cache cache = cache_of(c, a[2], a[3], true);
+    void* t = dense(c, a[4], "table_out", at::kInt, I2{p.S, c.cfg.max_pages});
+    void* r = dense(c, a[5], "ref_out", at::kInt, I1{c.cfg.n_pages});
+    void* u = dense(c, a[6], "n_used", at::kInt, I1{1});
+    return gto_pages_compact(c.handle, &p, &cache, static_cast<int32_t*>(t), static_cast<int32_t*>(r), static_cast<int32_t*>(u),
+                             stream_of(a[7]));
   });
 }
 
@@ -320,7 +433,8 @@ PyObject* make(PyObject*, PyObject* const* a, Py_ssize_t n) {
 
 #define GTO_FN(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(name)), METH_FASTCALL, nullptr}
 PyMethodDef kMethods[] = {GTO_FN(make),        GTO_FN(kv_append), GTO_FN(tree_attention),
-                          GTO_FN(verify_tree), GTO_FN(kv_commit), {nullptr, nullptr, 0, nullptr}};
+                          GTO_FN(verify_tree), GTO_FN(kv_commit), GTO_FN(sample_tokens), GTO_FN(verify_tree_limited),
+                          GTO_FN(pages_fork), GTO_FN(pages_resize), GTO_FN(pages_compact), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "_gto_decode", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -81,6 +81,54 @@ struct VerifyArgs {
 };
 cudaError_t launch_verify_tree(const VerifyArgs& a, int sms, cudaStream_t stream, int64_t* launches);
 
+// Rows to draw from, or trees to verify, under limits.
+struct LimitedArgs {
+  int N, V, dtype;       // sequences; length of a row
+  const char* logits;
+  int64_t row_stride;    // bytes
+  const float* temperature;
+  const int32_t* top_k;  // or null, as the next two
+  const float* top_p;
+  const float* min_p;
+  const float* u;        // of the drawn token
+  int32_t* token;        // [N], with trees [N, D+1]
+  int32_t* status;
+  // rows
+  const int32_t* rows;   // or null: row s
+  int n_rows;
+  float* logp;           // or null, as the next one
+  int32_t* n_kept;
+  // trees
+  int g, D, k, V_draft, rows_of_tree;
+  bool context_rows;
+  const int32_t* node_token;
+  const int32_t* node_parent;
+  const int32_t* node_depth;
+  const int32_t* node_slot;
+  const int32_t* n_nodes;
+  const int32_t* d2t;
+  const float* u_node;
+  int32_t* accept_len;
+  int32_t* path_node;
+};
+cudaError_t launch_limited(const LimitedArgs& a, bool tree, cudaStream_t stream, int64_t* launches);
+
+// Pages of the cache and the tables that name them.
+struct PoolArgs {
+  int S, page_size, n_pages, max_pages;
+  int32_t* page_table;
+  int32_t* kv_len;
+  int32_t* held;
+  int32_t* ref_count;
+  int32_t* status;
+};
+size_t pages_workspace(const gto_decode_config& c);
+cudaError_t launch_pages_fork(const PoolArgs& p, const int32_t* parent, void* ws, cudaStream_t stream, int64_t* launches);
+cudaError_t launch_pages_resize(const PoolArgs& p, const int32_t* want, const CacheArgs& c, void* ws, int sms,
+                                cudaStream_t stream, int64_t* launches);
+cudaError_t launch_pages_compact(const PoolArgs& p, const CacheArgs& c, int32_t* table_out, int32_t* ref_out, int32_t* n_used,
+                                 void* ws, int sms, cudaStream_t stream, int64_t* launches);
+
 struct AttnArgs {
   BatchArgs b;
   CacheArgs c;

@@ -122,6 +122,7 @@ const char* gto_status_string(gto_status s) {
     case GTO_ERR_TIMEOUT: return "a wait inside a kernel ran out";
     case GTO_ERR_TOO_LARGE: return "batch exceeds the fixed scratch of the no-allocation call";
     case GTO_ERR_BAD_INDEX: return "an index in a caller's table was out of range";
+    case GTO_ERR_NO_PAGES: return "too few free pages in the pool";
   }
   return "unknown status";
 }

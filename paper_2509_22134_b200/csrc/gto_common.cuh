@@ -15,6 +15,7 @@ constexpr unsigned kFull = 0xffffffffu;
 constexpr int kStatusNonFinite = 1;
 constexpr int kStatusBadIndex = 4;  // an index read from a caller's table was out of range
 constexpr int kStatusTimeout = 8;   // a bounded wait ran out
+constexpr int kStatusNoPages = 16;  // a page pool has no page left
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453094;
