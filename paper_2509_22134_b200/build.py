@@ -15,7 +15,7 @@ EXT = os.path.join(HERE, "_gto_decode.so")
 EXT_KEY = os.path.join(OBJ, "_gto_decode.key")  # what EXT was built for
 SOURCES = ["gto_api.cu", "row_reduce.cu", "tree_build.cu", "tree_reward.cu", "surrogate_grad.cu",
            "build_tree_noalloc.cu", "token_loss.cu", "decode_api.cu", "kv_cache.cu", "tree_verify.cu",
-           "tree_attention_simt.cu", "tree_attention_tc.cu", "limited_draw.cu", "page_pool.cu"]
+           "tree_attention_simt.cu", "tree_attention_tc.cu", "limited_bf16.cu", "limited_f16.cu", "limited_f32.cu", "page_pool.cu"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xptxas", "-v"]
 

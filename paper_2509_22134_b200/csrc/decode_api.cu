@@ -468,7 +468,7 @@ gto_status gto_sample_tokens(gto_decode_ctx* ctx, const void* logits, int64_t ro
   a.n_kept = n_kept;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return GTO_ERR_CUDA;
-  if (gto::launch_limited(a, false, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess) return GTO_ERR_CUDA;
+  if (gto::launch_limited(a, false, ctx->sms, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess) return GTO_ERR_CUDA;
   return GTO_OK;
 }
 
@@ -511,7 +511,7 @@ gto_status gto_verify_tree_limited(gto_decode_ctx* ctx, const gto_draft_tree* tr
   a.path_node = out->path_node;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return GTO_ERR_CUDA;
-  if (gto::launch_limited(a, true, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess) return GTO_ERR_CUDA;
+  if (gto::launch_limited(a, true, ctx->sms, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess) return GTO_ERR_CUDA;
   return GTO_OK;
 }
 

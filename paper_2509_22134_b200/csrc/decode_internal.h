@@ -111,7 +111,14 @@ struct LimitedArgs {
   int32_t* accept_len;
   int32_t* path_node;
 };
-cudaError_t launch_limited(const LimitedArgs& a, bool tree, cudaStream_t stream, int64_t* launches);
+cudaError_t launch_limited_bf16(const LimitedArgs& a, bool tree, int sms, cudaStream_t stream, int64_t* launches);
+cudaError_t launch_limited_f16(const LimitedArgs& a, bool tree, int sms, cudaStream_t stream, int64_t* launches);
+cudaError_t launch_limited_f32(const LimitedArgs& a, bool tree, int sms, cudaStream_t stream, int64_t* launches);
+inline cudaError_t launch_limited(const LimitedArgs& a, bool tree, int sms, cudaStream_t stream, int64_t* launches) {
+  if (a.dtype == GTO_BF16) return launch_limited_bf16(a, tree, sms, stream, launches);
+  if (a.dtype == GTO_F16) return launch_limited_f16(a, tree, sms, stream, launches);
+  return launch_limited_f32(a, tree, sms, stream, launches);
+}
 
 // Pages of the cache and the tables that name them.
 struct PoolArgs {

@@ -22,7 +22,7 @@
 // barrier for the exchange; 103 us with the row kept in shared memory, which left room for three
 // quarters of the clusters and took a second pass for the weights).
 #include "decode_common.cuh"
-#include "exp2_fp64.cuh"
+#include "logit_weights.cuh"
 
 namespace gto {
 namespace {
@@ -78,61 +78,7 @@ __device__ __forceinline__ double scan64(double v, int lane) {
   return v;
 }
 
-// The largest of 16 bytes of logits, of two packed 16-bit ones at a time; NaN if one of them is.
-template <typename T>
-__device__ __forceinline__ uint32_t max_word(uint32_t a, uint32_t b) {
-  uint32_t d;
-  if (T::kBytes == 4) asm("max.NaN.f32 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  else if (T::kNegInfElem == 0xff80u) asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  else asm("max.NaN.f16x2 %0, %1, %2;" : "=r"(d) : "r"(a), "r"(b));
-  return d;
-}
-template <typename T>
-__device__ __forceinline__ uint32_t max_of(const uint4& v) {
-  return max_word<T>(max_word<T>(v.x, v.y), max_word<T>(v.z, v.w));
-}
-template <typename T>
-__device__ __forceinline__ float max_half(uint32_t w) {  // of the word's two halves
-  if (T::kBytes == 4) return __uint_as_float(w);
-  w = max_word<T>(w, __byte_perm(w, w, 0x1032));
-  return T::load1(&w, 0);
-}
-
-// Sum of the weights of 16 bytes of logits, 2^((f - m) c2), in fp32: pairs side by side.
-template <typename T>
-__device__ __forceinline__ float weights(const uint4& v, float m, float c2) {
-  constexpr int E = T::kPerVec;
-  float f[E];
-  T::unpack(v, f);
-  uint64_t neg, scale, sum[E / 2];
-  asm("mov.b64 %0, {%1, %1};" : "=l"(neg) : "f"(-m));
-  asm("mov.b64 %0, {%1, %1};" : "=l"(scale) : "f"(c2));
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) {
-    float a, b;
-    asm("{\n .reg .b64 x;\n mov.b64 x, {%2, %3};\n add.rn.f32x2 x, x, %4;\n mul.rn.f32x2 x, x, %5;\n mov.b64 {%0, %1}, x;\n}"
-        : "=f"(a), "=f"(b)
-        : "f"(f[2 * e]), "f"(f[2 * e + 1]), "l"(neg), "l"(scale));
-    a = ex2_approx(a);
-    b = ex2_approx(b);
-    asm("mov.b64 %0, {%1, %2};" : "=l"(sum[e]) : "f"(a), "f"(b));
-  }
-#pragma unroll
-  for (int w = E / 4; w > 0; w /= 2)
-#pragma unroll
-    for (int e = 0; e < w; ++e) asm("add.rn.f32x2 %0, %1, %2;" : "=l"(sum[e]) : "l"(sum[e]), "l"(sum[e + w]));
-  float a, b;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(sum[0]));
-  return a + b;
-}
-
 // ---- what a CTA tells the others: a store into their shared memory that their barrier counts
-__device__ __forceinline__ uint32_t smem_of(const void* p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
-__device__ __forceinline__ uint32_t in_cta(uint32_t addr, int cta) {
-  uint32_t r;
-  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(r) : "r"(addr), "r"(cta));
-  return r;
-}
 __device__ __forceinline__ void tell(uint32_t to, uint64_t a, uint64_t b, uint32_t bar) {
   asm volatile("st.async.weak.shared::cluster.mbarrier::complete_tx::bytes.v2.b64 [%0], {%1, %2}, [%3];" ::"r"(to), "l"(a),
                "l"(b), "r"(bar)
