@@ -17,6 +17,8 @@
 // it could turn is taken again after the row has been summed in fp64.
 #pragma once
 
+#include <algorithm>
+
 #include "limited_row.cuh"
 
 namespace gto {
@@ -27,10 +29,10 @@ constexpr int kLater = -2;  // token of a row that is left to the second kernel
 enum Mode { kEasy, kAll, kLeft };
 
 // Row (kTree: tree) s, by the CTAs of a cluster.
-template <typename T, int kCluster, bool kTree, Mode kMode>
-__device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kMode != kEasy>& sh, int s, int rank) {
+template <typename T, int kCluster, int kThreads, bool kTree, Mode kMode>
+__device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kThreads, kMode != kEasy>& sh, int s, int rank) {
   constexpr bool kServesAll = kMode != kEasy;
-  using R = Row<T, kCluster, kServesAll>;
+  using R = Row<T, kCluster, kThreads, kServesAll>;
   constexpr int kNodes = kTree ? kMaxNodes : 1;
   constexpr int kChunks = kMaxNodes / 32;
   __shared__ int s_id[kNodes], s_parent[kNodes], s_removed[kNodes];
@@ -379,23 +381,27 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kMo
 }
 
 // One CTA a row, for many rows: what a list of the likeliest tokens, or the sums of the warps, can tell.
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 5) many_rows_kernel(LimitedArgs a) {
-  __shared__ Shared<1, false> sh;
-  serve<T, 1, false, kEasy>(a, sh, static_cast<int>(blockIdx.x), 0);
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1280 / kThreads) many_rows_kernel(LimitedArgs a) {
+  __shared__ Shared<1, kThreads, false> sh;
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the next kernel may get ready)
+  serve<T, 1, kThreads, false, kEasy>(a, sh, static_cast<int>(blockIdx.x), 0);
 }
+
+constexpr int kClusterThreads = 256;
 
 // A cluster a row or tree, for whatever the limits leave.
 template <typename T, int kCluster, bool kTree>
-__global__ void __launch_bounds__(kThreads, 2) limited_kernel(LimitedArgs a) {
-  __shared__ Shared<kCluster, true> sh;
-  serve<T, kCluster, kTree, kAll>(a, sh, static_cast<int>(blockIdx.x / kCluster), static_cast<int>(blockIdx.x % kCluster));
+__global__ void __launch_bounds__(kClusterThreads, 2) limited_kernel(LimitedArgs a) {
+  __shared__ Shared<kCluster, kClusterThreads, true> sh;
+  serve<T, kCluster, kClusterThreads, kTree, kAll>(a, sh, static_cast<int>(blockIdx.x / kCluster), static_cast<int>(blockIdx.x % kCluster));
 }
 
 // The rows that many_rows_kernel has left, those of a cluster a fixed share of all.
 template <typename T, int kCluster>
-__global__ void __launch_bounds__(kThreads, 2) left_rows_kernel(LimitedArgs a) {
-  __shared__ Shared<kCluster, true> sh;
+__global__ void __launch_bounds__(kClusterThreads, 2) left_rows_kernel(LimitedArgs a) {
+  __shared__ Shared<kCluster, kClusterThreads, true> sh;
+  asm volatile("griddepcontrol.wait;" ::: "memory");
   const int rank = static_cast<int>(blockIdx.x % kCluster), clusters = static_cast<int>(gridDim.x / kCluster);
   const int lane = threadIdx.x & 31;
   for (int64_t s0 = blockIdx.x / kCluster; s0 < a.N; s0 += 32ll * clusters) {
@@ -405,39 +411,46 @@ __global__ void __launch_bounds__(kThreads, 2) left_rows_kernel(LimitedArgs a) {
     while (left) {
       const int at = __ffs(left) - 1;
       left &= left - 1;
-      serve<T, kCluster, false, kLeft>(a, sh, static_cast<int>(s0 + static_cast<int64_t>(at) * clusters), rank);
+      serve<T, kCluster, kClusterThreads, false, kLeft>(a, sh, static_cast<int>(s0 + static_cast<int64_t>(at) * clusters), rank);
     }
   }
 }
 
 template <typename K>
-cudaError_t launch(K kernel, const LimitedArgs& a, unsigned grid, int cluster, cudaStream_t stream, int64_t* launches) {
+cudaError_t launch(K kernel, const LimitedArgs& a, int64_t rows, int cluster, int threads, bool after, cudaStream_t stream,
+                   int64_t* launches) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(grid);
-  cfg.blockDim = dim3(kThreads);
+  cfg.gridDim = dim3(static_cast<unsigned>(rows * cluster));
+  cfg.blockDim = dim3(static_cast<unsigned>(threads));
   cfg.stream = stream;
-  cudaLaunchAttribute attr{};
-  attr.id = cudaLaunchAttributeClusterDimension;
-  attr.val.clusterDim.x = static_cast<unsigned>(cluster);
-  attr.val.clusterDim.y = 1;
-  attr.val.clusterDim.z = 1;
-  cfg.attrs = &attr;
-  cfg.numAttrs = 1;
+  cudaLaunchAttribute attr[2] = {};
+  attr[0].id = cudaLaunchAttributeClusterDimension;
+  attr[0].val.clusterDim.x = static_cast<unsigned>(cluster);
+  attr[0].val.clusterDim.y = 1;
+  attr[0].val.clusterDim.z = 1;
+  // (its CTAs may be placed while the kernel before it ends, for which they wait themselves)
+  attr[1].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr[1].val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = attr;
+  cfg.numAttrs = after ? 2 : 1;
   ++*launches;
   return cudaLaunchKernelEx(&cfg, kernel, a);
 }
 
 template <typename T>
 cudaError_t limited_as(const LimitedArgs& a, bool tree, int sms, cudaStream_t stream, int64_t* launches) {
-  if (tree) return launch(limited_kernel<T, 8, true>, a, static_cast<unsigned>(a.N) * 8, 8, stream, launches);
+  if (tree) return launch(limited_kernel<T, 8, true>, a, a.N, 8, kClusterThreads, false, stream, launches);
   // As many CTAs a row as fit the device twice over; one where there are rows enough, and then the few that need more
   // than it can tell by clusters.
-  if (a.N * 8ll <= 2ll * sms) return launch(limited_kernel<T, 8, false>, a, static_cast<unsigned>(a.N) * 8, 8, stream, launches);
-  if (a.N * 4ll <= 2ll * sms) return launch(limited_kernel<T, 4, false>, a, static_cast<unsigned>(a.N) * 4, 4, stream, launches);
-  const cudaError_t e = launch(many_rows_kernel<T>, a, static_cast<unsigned>(a.N), 1, stream, launches);
+  if (a.N * 8ll <= 2ll * sms) return launch(limited_kernel<T, 8, false>, a, a.N, 8, kClusterThreads, false, stream, launches);
+  if (a.N * 4ll <= 2ll * sms) return launch(limited_kernel<T, 4, false>, a, a.N, 4, kClusterThreads, false, stream, launches);
+  // (ten small CTAs an SM where they have work, else five with as many loads on their way)
+  const bool small = a.N > 5ll * sms;
+  const cudaError_t e = small ? launch(many_rows_kernel<T, 128>, a, a.N, 1, 128, false, stream, launches)
+                              : launch(many_rows_kernel<T, 256>, a, a.N, 1, 256, false, stream, launches);
   if (e != cudaSuccess) return e;
-  const int clusters = sms * 2 / 8;  // (an odd number on a B200: settings that repeat fall to all)
-  return launch(left_rows_kernel<T, 8>, a, static_cast<unsigned>(clusters) * 8, 8, stream, launches);
+  // (73 clusters on a B200: a number by which settings that repeat fall to all)
+  return launch(left_rows_kernel<T, 4>, a, std::max(sms * 2 / 4 - 1, 1), 4, kClusterThreads, true, stream, launches);
 }
 
 }  // namespace gto

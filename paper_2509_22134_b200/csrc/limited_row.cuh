@@ -6,12 +6,9 @@
 
 namespace gto {
 
-constexpr int kThreads = 256;
-constexpr int kWarps = kThreads / 32;
 constexpr int kUnroll = 4;              // vectors of 16 bytes a thread takes in a step
-constexpr int kBins = 512;              // of the slots' maxima, by their distance from the row's
+constexpr int kBins = 128;              // of the slots' maxima, by their distance from the row's
 constexpr int kWideBins = 2048;         // of the tokens, where more stays than a list holds
-constexpr int kItems = 96;              // slots that a warp reads again
 
 // How far a sum of fp32 weights can be from the true one, relative to the row's whole mass.  A weight 2^-a is off by
 // 2^-22 (the exponential) and 2^-24 a ln 2 (rounding of z - ref; the rest of the argument is carried in two words)
@@ -127,11 +124,13 @@ struct Cut {
   bool close;       // the row's mass is not exact enough to tell
 };
 
-// kCluster CTAs a row.  kServesAll: rows of which much stays are served too, by lists twice as long.
-template <int kCluster, bool kServesAll>
+// kCluster CTAs of kThreads a row.  kServesAll: rows of which much stays are served too, by lists twice as long.
+template <int kCluster, int kThreads, bool kServesAll>
 struct Shared {
+  static constexpr int kWarps = kThreads / 32;
   static constexpr int kSlots = kServesAll ? 16 : 8;      // maxima that a thread leaves, of one step or several
   static constexpr int kList = kServesAll ? 1024 : 512;   // tokens that a list holds
+  static constexpr int kItems = 768 / kWarps;             // slots that a warp reads again
   static constexpr int kMaxSteps = static_cast<int>(kMaxTargetRow / 16 / (kThreads * kUnroll)) / kCluster;
   union {
     uint16_t top[kSlots][kThreads];
@@ -152,7 +151,6 @@ struct Shared {
   double group[kMaxSteps];
   uint16_t items[kWarps][kItems];
   alignas(16) int bins[kBins];
-  alignas(16) int bins_all[kCluster > 1 ? kBins : 4];
   Mail mail[2][kCluster * kWarps];
   double red[2][kWarps];
   int red_n[2][kWarps];
@@ -165,11 +163,12 @@ struct Shared {
 
 // A CTA's share of a row: of the row's blocks of kThreads vectors every kCluster-th, so that tokens fall to threads
 // by chance wherever the likely ones stand.
-template <typename T, int kCluster, bool kServesAll>
+template <typename T, int kCluster, int kThreads, bool kServesAll>
 struct Row {
-  using Mem = Shared<kCluster, kServesAll>;
+  using Mem = Shared<kCluster, kThreads, kServesAll>;
+  static constexpr int kWarps = Mem::kWarps;
   static constexpr int E = T::kPerVec;
-  static constexpr int kSlots = Mem::kSlots, kList = Mem::kList, kMaxSteps = Mem::kMaxSteps;
+  static constexpr int kSlots = Mem::kSlots, kList = Mem::kList, kMaxSteps = Mem::kMaxSteps, kItems = Mem::kItems;
   static constexpr int kAim = kList * 5 / 6;  // tokens that a list is made for
   static constexpr int kEach = kList / kThreads;
   static constexpr int kMails = kCluster * kWarps;
@@ -343,7 +342,7 @@ struct Row {
     bool bad = false, low = false;
     int slot = 0, in_slot = 0;
     // (what the next steps count in, behind the barrier below)
-    sh.bins[tid] = sh.bins[tid + kThreads] = 0;
+    if (tid < kBins) sh.bins[tid] = 0;
     if (tid == 0) sh.n_list = 0;
 #pragma unroll 1
     for (int step = 0; step < steps; ++step) {
@@ -441,16 +440,29 @@ struct Row {
     }
     if (n > kItems) return false;
     __syncwarp();
-    for (int i = lane; i < n * each_item; i += 32) {
-      const int item = sh.items[warp][i / each_item];
-      const int at = vec_of((item >> 8) * each_item + i % each_item, item & 255);
-      if (at >= nvec) continue;
-      const uint4 v = load(at);
-      float x[E];
-      T::unpack(v, x);
+    constexpr int kAtOnce = 4;
+    for (int i0 = lane; i0 < n * each_item; i0 += 32 * kAtOnce) {
+      uint4 v[kAtOnce];
+      int at[kAtOnce];
 #pragma unroll
-      for (int e = 0; e < E; ++e)
-        if (x[e] >= tau) f(x[e], at * E + e);
+      for (int u = 0; u < kAtOnce; ++u) {
+        const int i = i0 + 32 * u;
+        at[u] = nvec;
+        if (i < n * each_item) {
+          const int item = sh.items[warp][i / each_item];
+          at[u] = vec_of((item >> 8) * each_item + i % each_item, item & 255);
+        }
+        if (at[u] < nvec) v[u] = load(at[u]);
+      }
+#pragma unroll
+      for (int u = 0; u < kAtOnce; ++u) {
+        if (at[u] >= nvec || !(max_half<T>(max_of<T>(v[u])) >= tau)) continue;
+        float x[E];
+        T::unpack(v[u], x);
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if (x[e] >= tau) f(x[e], at[u] * E + e);
+      }
     }
     __syncwarp();
     return true;
@@ -475,54 +487,43 @@ struct Row {
     for (int s = 0; s < slots; ++s) {
       const float top = from16(sh.top[s][tid]);
       if (top == -INFINITY) continue;
-      const float x = fmaxf((M - top) * unit, 0.f);  // up to 8: bins of 1/32; from there up to 40 of 1/8
-      const int b = x < 8.f ? static_cast<int>(x * 32.f) : x < 40.f ? 256 + static_cast<int>((x - 8.f) * 8.f) : kBins;
+      const float x = fmaxf((M - top) * unit, 0.f);  // up to 8: bins of 1/8; from there up to 40 of 1/2
+      const int b = x < 8.f ? static_cast<int>(x * 8.f) : x < 40.f ? 64 + static_cast<int>((x - 8.f) * 2.f) : kBins;
       if (b < kBins) atomicAdd(&sh.bins[b], 1);
     }
     cluster_sync();
-    const int* bins = sh.bins;
-    if (kCluster > 1) {
-      int n0 = 0, n1 = 0;
-#pragma unroll
-      for (int d = 0; d < kCluster; ++d) {
-        const uint64_t two = far_u64(&sh.bins[2 * tid], d);
-        n0 += static_cast<int>(two);
-        n1 += static_cast<int>(two >> 32);
-      }
-      sh.bins_all[2 * tid] = n0;
-      sh.bins_all[2 * tid + 1] = n1;
-      __syncthreads();
-      bins = sh.bins_all;
-    }
     if (warp == 0) {
       constexpr int kOf = kBins / 32;
-      const auto reaches = [](int b) { return b < 256 ? static_cast<float>(b) * (1.f / 32) : 8.f + static_cast<float>(b - 256) * (1.f / 8); };
-      const float buckets = static_cast<float>(nvec) / static_cast<float>(kUnroll * per_slot);
-      const auto tokens = [&](int j) { return -buckets * __logf(1.f - fminf(static_cast<float>(j) / buckets, 0.995f)); };
+      const auto reaches = [](int b) { return b < 64 ? static_cast<float>(b) * (1.f / 8) : 8.f + static_cast<float>(b - 64) * (1.f / 2); };
+      const float buckets = static_cast<float>(nvec) / static_cast<float>(kUnroll * per_slot), bucket = 1.f / buckets;
+      const auto tokens = [&](int j) { return -buckets * __logf(1.f - fminf(static_cast<float>(j) * bucket, 0.995f)); };
       // slots, then tokens, then mass, up to each bin
-      int n[kOf], sum = 0;
+      int n[kOf] = {0, 0, 0, 0};
 #pragma unroll
-      for (int i = 0; i < kOf; i += 4) {
-        const int4 q = *reinterpret_cast<const int4*>(bins + lane * kOf + i);
-        n[i] = q.x;
-        n[i + 1] = q.y;
-        n[i + 2] = q.z;
-        n[i + 3] = q.w;
-        sum += q.x + q.y + q.z + q.w;
+      for (int d = 0; d < kCluster; ++d) {
+        if (kCluster == 1) {
+          const int4 q = *reinterpret_cast<const int4*>(sh.bins + lane * kOf);
+          n[0] = q.x, n[1] = q.y, n[2] = q.z, n[3] = q.w;
+        } else {
+          const uint64_t q0 = far_u64(&sh.bins[lane * kOf], d), q1 = far_u64(&sh.bins[lane * kOf + 2], d);
+          n[0] += static_cast<int>(q0), n[1] += static_cast<int>(q0 >> 32), n[2] += static_cast<int>(q1), n[3] += static_cast<int>(q1 >> 32);
+        }
       }
-      int j = scan_warp(sum, lane) - sum;
-      const int j0 = j;
-      float t = tokens(j), m = 0.f;
+      int j = n[0] + n[1] + n[2] + n[3];
+      j = scan_warp(j, lane) - j;
+      float t[kOf], m[kOf], before = tokens(j), sum = 0.f;
+      bool k_enough[kOf];
 #pragma unroll
       for (int i = 0; i < kOf; ++i) {
         const int b = lane * kOf + i;
-        if (n[i] == 0) continue;
         j += n[i];
-        const float next = tokens(j);
-        m += (next - t) * ex2_approx(-0.5f * (reaches(b) + reaches(b + 1)));
-        t = next;
+        k_enough[i] = j >= top_k;
+        t[i] = tokens(j);
+        sum += (t[i] - before) * ex2_approx(-0.5f * (reaches(b) + reaches(b + 1)));
+        m[i] = sum;
+        before = t[i];
       }
-      const float m0 = scan_warp(m, lane) - m;
+      const float m0 = scan_warp(sum, lane) - sum;
       // the first bin that is enough for one of the limits
       const bool k = top_k > 0, p = top_p < 1.f && !k;
       const float goal = p ? static_cast<float>(mass * (top_p + 0.1 * (1.0 - top_p))) : 0.f;
@@ -530,21 +531,12 @@ struct Row {
       const float x_floor = floor > 0.f && !(k && top_p < 1.f) ? -__log2f(floor) * 1.001f + 1e-3f : INFINITY;
       int found = kBins;
       float expect = 0.f;
-      j = j0;
-      t = tokens(j);
-      m = m0;
 #pragma unroll
-      for (int i = 0; i < kOf; ++i) {
+      for (int i = kOf - 1; i >= 0; --i) {
         const int b = lane * kOf + i;
-        if (n[i] > 0) {
-          j += n[i];
-          const float next = tokens(j);
-          m += (next - t) * ex2_approx(-0.5f * (reaches(b) + reaches(b + 1)));
-          t = next;
-        }
-        if (found == kBins && ((k && j >= top_k) || (p && m >= goal) || reaches(b + 1) >= x_floor)) {
+        if ((k && k_enough[i]) || (p && m0 + m[i] >= goal) || reaches(b + 1) >= x_floor) {
           found = b;
-          expect = t;
+          expect = t[i];
         }
       }
       const unsigned any = __ballot_sync(kFull, found < kBins);
@@ -586,9 +578,16 @@ struct Row {
     }
     from[kCluster] = total;
     if (total <= kList) {
+      for (int i = tid; i < total; i += kThreads) {
+        int of = 0;
 #pragma unroll
-      for (int d = 0; d < kCluster; ++d)
-        for (int i = tid; i < from[d + 1] - from[d]; i += kThreads) sh.merged[from[d] + i] = far_u64(&sh.list[i], d);
+        for (int d = 1; d < kCluster; ++d) of += i >= from[d];
+        int first = 0;
+#pragma unroll
+        for (int d = 1; d < kCluster; ++d)
+          if (d == of) first = from[d];
+        sh.merged[i] = far_u64(&sh.list[i - first], of);
+      }
     }
     __syncthreads();
     return total;
@@ -977,17 +976,19 @@ struct Row {
     float x[E];
     T::unpack(mv, x);
     double acc = start;
+    float found = 0.f;
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int id = i * E + e;
       const double y = out(id) ? 0.0 : static_cast<double>(fine_weight(x[e] - M, c));
       if (f.id < 0 && y > 0.0 && acc + y > aim) {
         f.id = id;
-        f.weight = raw(x[e]);
+        found = x[e];
         f.close = aim - acc < slack || acc + y - aim < slack;
       }
       acc += y;
     }
+    f.weight = raw(found);
     return f;
   }
 
@@ -1216,6 +1217,8 @@ struct Row {
         hi2 = hi;
       }
     }
+    const float f_lo = from_orderable(lo), f_lo2 = two ? from_orderable(lo2) : INFINITY;
+    const float f_hi = hi == 0xffffffffu ? INFINITY : from_orderable(hi), f_hi2 = hi2 == 0xffffffffu ? INFINITY : from_orderable(hi2);
     if (tid == 0) sh.n_list = 0;
     __syncthreads();
     // ---- the pass in fp64: mass and number above the interval, and above the second one (without top-k: of all)
@@ -1227,13 +1230,12 @@ struct Row {
       raw_of(v, x, w);
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const uint32_t key = orderable(x[e]);
-        const bool a1 = key > hi, a2 = key > hi2;
+        const bool a1 = x[e] > f_hi, a2 = x[e] > f_hi2;
         above += a1 ? w[e] : 0.0;
         above2 += a2 ? w[e] : 0.0;
         n_above += a1;
         n_above2 += a2;
-        if ((key >= lo && key <= hi) || (key >= lo2 && key <= hi2)) {
+        if ((!a1 && x[e] >= f_lo) || (!a2 && x[e] >= f_lo2)) {
           const int i = atomicAdd(&sh.n_list, 1);
           if (i < kList) sh.list[i] = make_key(x[e], at * E + e);
         }
