@@ -42,6 +42,7 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
   const int tid = threadIdx.x, lane = tid & 31;
   R row(sh, a.V, rank);
   const bool first = row.rank == 0 && tid == 0;
+  if constexpr (kServesAll) row.fill_table();  // (read behind a barrier)
 
   const float heat = a.temperature[s];
   const bool greedy = heat == 0.f;
@@ -358,7 +359,7 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
     if constexpr (kServesAll) {
       if (close) {
         Found f;
-        if (!kTree && !limited) f = row.locate([&](float x, int) { return row.raw(x); }, u_last, 0.0);
+        if (!kTree && !limited) f = row.locate_all(u_last);
         else f = row.locate(left, u_last, 0.0);
         write(f, f.total);
       }

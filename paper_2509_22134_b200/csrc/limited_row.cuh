@@ -159,6 +159,7 @@ struct Shared {
   uint32_t key_lo, key_hi;
   double value, value2;
   Cut cut;
+  double pow2[kServesAll ? 32 : 1];  // 2^(j/32)
 };
 
 // A CTA's share of a row: of the row's blocks of kThreads vectors every kCluster-th, so that tokens fall to threads
@@ -213,6 +214,31 @@ struct Row {
   __device__ __forceinline__ uint4 load(int v) const { return ld_stream16(z + static_cast<int64_t>(v) * 16); }
   __device__ __forceinline__ double raw(float x) const {
     return exp2_neg((static_cast<double>(x) - static_cast<double>(M)) * scale);
+  }
+
+  __device__ __forceinline__ void fill_table() {
+    if (tid < 32) sh.pow2[tid] = 2.0 * exp2_neg(tid * (1.0 / 32) - 1.0);
+  }
+  // As raw(), for many tokens, and only where the weight is at least 2^-1000 (a number without meaning elsewhere): 2^x = 2^e 2^(j/32) 2^f
+  // with |f| <= 1/64, whose polynomial of degree 5 (through the Chebyshev points of (2^f - 1) / f) is off by 1.4e-16.
+  __device__ __forceinline__ double raw_near(float x) const {
+    constexpr double kMagic = 211106232532992.0;  // 1.5 * 2^47: 32 x in the low bits
+    const double d = static_cast<double>(x) - static_cast<double>(M);
+    const double t = fma(d, scale, kMagic);
+    const double f = fma(d, scale, -(t - kMagic));
+    double y = 0.0013333604694153824;
+    y = fma(y, f, 0.009618176115571158);
+    y = fma(y, f, 0.05550410866453748);
+    y = fma(y, f, 0.24022650695623157);
+    y = fma(y, f, 0.6931471805599453);
+    y = fma(y, f, 1.0);
+    const int k = __double2loint(t);
+    y *= sh.pow2[k & 31];
+    return __hiloint2double(__double2hiint(y) + ((k >> 5) << 20), __double2loint(y));
+  }
+  // The value from which on it serves.
+  __device__ __forceinline__ float near_from() const {
+    return fmaxf(static_cast<float>(static_cast<double>(M) - 999.0 / scale), -3.4028235e38f);
   }
 
   // f(vector, its number) over the thread's vectors; the next three are on their way meanwhile.
@@ -1007,19 +1033,22 @@ struct Row {
     run_of(&lo, &hi);
     ahead([&](int i) { return lo + i; }, hi - lo, f);
   }
-  // fp64 weights of the tokens of a vector.
-  __device__ __forceinline__ void raw_of(const uint4& v, float (&x)[E], double (&w)[E]) const {
+  // fp64 weights of the tokens of a vector; from: near_from().
+  __device__ __forceinline__ void raw_of(const uint4& v, float from, float (&x)[E], double (&w)[E]) const {
     T::unpack(v, x);
 #pragma unroll
-    for (int e = 0; e < E; ++e) w[e] = raw(x[e]);
+    for (int e = 0; e < E; ++e) w[e] = raw_near(x[e]);
+#pragma unroll
+    for (int e = 0; e < E; ++e) w[e] = x[e] >= from ? w[e] : 0.0;
   }
   // The row's mass in fp64.
   __device__ __forceinline__ double whole() {
     double m[2] = {0.0, 0.0};
+    const float from = near_from();
     vectors([&](const uint4& v, int) {
       float x[E];
       double w[E];
-      raw_of(v, x, w);
+      raw_of(v, from, x, w);
 #pragma unroll
       for (int e = 0; e < E; ++e) m[e & 1] += w[e];
     });
@@ -1084,6 +1113,20 @@ struct Row {
       for (int e = 0; e < E; ++e) mine += w[e];
     });
     return pick(mine, weight, u, aim);
+  }
+
+  // The token of a row of which all stays, in fp64.
+  __device__ __forceinline__ Found locate_all(double u) {
+    double m[2] = {0.0, 0.0};
+    const float from = near_from();
+    along([&](const uint4& v, int) {
+      float x[E];
+      double w[E];
+      raw_of(v, from, x, w);
+#pragma unroll
+      for (int e = 0; e < E; ++e) m[e & 1] += w[e];
+    });
+    return pick(m[0] + m[1], [&](float x, int) { return raw(x); }, u, 0.0);
   }
 
   // ---- rows of which more stays than a list holds: the tokens are counted by their distance from the largest logit, which
@@ -1197,14 +1240,14 @@ struct Row {
     const int b = min(min(b_k, b_p), b_m);
     const bool two = k && p;  // the mass of the first top_k is needed, whatever binds
     if (b >= kWideBins - 1 || (two && b_k >= kWideBins - 1)) return;
-    int near = b == b_p ? static_cast<int>(sh.wide[b]) : 0;  // (a count is exact)
-    if (b == b_m) near |= (x_floor - b < 0.02f ? 1 : 0) | (x_floor - b > 0.98f ? 2 : 0);
+    int edge = b == b_p ? static_cast<int>(sh.wide[b]) : 0;  // (a count is exact)
+    if (b == b_m) edge |= (x_floor - b < 0.02f ? 1 : 0) | (x_floor - b > 0.98f ? 2 : 0);
     const int held = sh.wide_n[b] + (two ? sh.wide_n[b_k] : 0);
-    const int up = near & 1 && b > 0 ? sh.wide_n[b - 1] : 0, down = near & 2 ? sh.wide_n[b + 1] : 0;
+    const int up = edge & 1 && b > 0 ? sh.wide_n[b - 1] : 0, down = edge & 2 ? sh.wide_n[b + 1] : 0;
     int b0 = b, b1 = b;
     if (held + up + down <= kAim) {
-      if (near & 1) b0 = max(b - 1, 0);
-      if (near & 2) b1 = min(b + 1, kWideBins - 2);
+      if (edge & 1) b0 = max(b - 1, 0);
+      if (edge & 2) b1 = min(b + 1, kWideBins - 2);
     }
     uint32_t lo, hi, lo2 = 0xffffffffu, hi2 = orderable(-INFINITY);  // (the second one holds nothing)
     interval(b0, b1, &lo, &hi);
@@ -1224,27 +1267,41 @@ struct Row {
     // ---- the pass in fp64: mass and number above the interval, and above the second one (without top-k: of all)
     double above = 0.0, above2 = 0.0;
     int n_above = 0, n_above2 = 0;
+    const float near = near_from();
     along([&](const uint4& v, int at) {
       float x[E];
       double w[E];
-      raw_of(v, x, w);
+      raw_of(v, near, x, w);
+      bool in = false;
 #pragma unroll
       for (int e = 0; e < E; ++e) {
-        const bool a1 = x[e] > f_hi, a2 = x[e] > f_hi2;
+        const bool a1 = x[e] > f_hi;
         above += a1 ? w[e] : 0.0;
-        above2 += a2 ? w[e] : 0.0;
         n_above += a1;
-        n_above2 += a2;
-        if ((!a1 && x[e] >= f_lo) || (!a2 && x[e] >= f_lo2)) {
-          const int i = atomicAdd(&sh.n_list, 1);
-          if (i < kList) sh.list[i] = make_key(x[e], at * E + e);
+        in |= !a1 && x[e] >= f_lo;
+      }
+      if (p) {
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const bool a2 = x[e] > f_hi2;
+          above2 += a2 ? w[e] : 0.0;
+          n_above2 += a2;
+          in |= !a2 && x[e] >= f_lo2;
         }
+      }
+      if (in) {
+#pragma unroll
+        for (int e = 0; e < E; ++e)
+          if ((x[e] >= f_lo && x[e] <= f_hi) || (x[e] >= f_lo2 && x[e] <= f_hi2)) {
+            const int i = atomicAdd(&sh.n_list, 1);
+            if (i < kList) sh.list[i] = make_key(x[e], at * E + e);
+          }
       }
     });
     out->run = above;
     const Mail r = reduce(above, above2, n_above, n_above2);
     const int n_all = join();
-    if (n_all > kList || n_all == 0) return;
+    if (n_all > kList) return;
     uint64_t* list = tokens();
     sort(list, n_all);
     // ---- the list: first the interval's, then (with both limits) the second one's
@@ -1314,10 +1371,15 @@ struct Row {
       higher |= r.n > 0 && r.a >= goal;
     }
     if (floor > 0.f) {
-      if (heavy < first_n) stay = min(stay, heavy);
-      higher |= heavy == 0;
+      if (heavy < first_n || raw(from_orderable(lo)) < static_cast<double>(floor)) stay = min(stay, heavy);
+      higher |= heavy == 0 && (r.n == 0 || raw(f_hi) < static_cast<double>(floor));
     }
     if (higher || stay > first_n) return;
+    __syncthreads();
+    if (tid == 0) {  // (of the interval none: what lies above it)
+      sh.value = r.a;
+      sh.cut.border = static_cast<uint64_t>(hi) + 1 << 32;
+    }
     __syncthreads();
     acc = r.a + before;
 #pragma unroll
