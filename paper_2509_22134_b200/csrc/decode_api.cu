@@ -16,6 +16,7 @@ struct gto_decode_ctx {
   int32_t* status;
   char* attn_ws;     // parts of blocks that were cut, null where the tensor-core kernel does not serve
   char* pages_ws;    // plans of the page calls, null without GTO_DECODE_PAGES
+  int32_t* left;     // rows that gto_sample_tokens leaves to its second kernel, with V_target only
   int64_t launches;
 };
 
@@ -246,7 +247,8 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
   const bool tc = c->n_kv_heads > 0 && gto::attention_tc_serves(*c);
   const size_t attn = tc ? (gto::attention_tc_workspace(*c, ctx->sms) + 255) / 256 * 256 : 0;
   const size_t pages = (c->flags & GTO_DECODE_PAGES) ? gto::pages_workspace(*c) : 0;
-  if (cudaMalloc(&ctx->ws, 256 + attn + pages) != cudaSuccess) {
+  const size_t left = c->V_target > 0 ? sizeof(int32_t) * (gto::kLeftRows + gto::kMaxLeft) : 0;
+  if (cudaMalloc(&ctx->ws, 256 + attn + pages + left) != cudaSuccess) {
     cudaGetLastError();
     delete ctx;
     return GTO_ERR_WORKSPACE;
@@ -254,8 +256,10 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
   ctx->status = reinterpret_cast<int32_t*>(ctx->ws);
   ctx->attn_ws = tc ? ctx->ws + 256 : nullptr;
   ctx->pages_ws = (c->flags & GTO_DECODE_PAGES) ? ctx->ws + 256 + attn : nullptr;
+  ctx->left = reinterpret_cast<int32_t*>(ctx->ws + 256 + attn + pages);
   // (waited for: the first call may come on a stream that the default one does not order)
-  if (cudaMemset(ctx->ws, 0, 256) != cudaSuccess || cudaStreamSynchronize(nullptr) != cudaSuccess) {
+  if (cudaMemset(ctx->ws, 0, 256) != cudaSuccess || (left > 0 && cudaMemset(ctx->left, 0, 256) != cudaSuccess) ||
+      cudaStreamSynchronize(nullptr) != cudaSuccess) {
     cudaGetLastError();
     cudaFree(ctx->ws);
     delete ctx;
@@ -466,6 +470,7 @@ gto_status gto_sample_tokens(gto_decode_ctx* ctx, const void* logits, int64_t ro
   a.n_rows = n_rows;
   a.logp = logp;
   a.n_kept = n_kept;
+  a.left = ctx->left;
   DeviceGuard guard(ctx->device);
   if (!guard.ok) return GTO_ERR_CUDA;
   if (gto::launch_limited(a, false, ctx->sms, static_cast<cudaStream_t>(stream), &ctx->launches) != cudaSuccess) return GTO_ERR_CUDA;

@@ -81,6 +81,9 @@ struct VerifyArgs {
 };
 cudaError_t launch_verify_tree(const VerifyArgs& a, int sms, cudaStream_t stream, int64_t* launches);
 
+constexpr int kMaxLeft = 4096;  // rows that gto_sample_tokens can list for its second kernel,
+constexpr int kLeftRows = 64;   // from this word of their workspace on
+
 // Rows to draw from, or trees to verify, under limits.
 struct LimitedArgs {
   int N, V, dtype;       // sequences; length of a row
@@ -98,6 +101,7 @@ struct LimitedArgs {
   int n_rows;
   float* logp;           // or null, as the next one
   int32_t* n_kept;
+  int32_t* left;         // workspace: their count, the CTAs that have read it (both 0 between calls), the rows
   // trees
   int g, D, k, V_draft, rows_of_tree;
   bool context_rows;

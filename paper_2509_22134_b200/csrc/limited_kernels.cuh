@@ -25,6 +25,13 @@ namespace gto {
 
 constexpr int kLater = -2;  // token of a row that is left to the second kernel
 
+// Marks a row as left, and lists it where there is room.
+__device__ __forceinline__ void leave(const LimitedArgs& a, int s) {
+  a.token[s] = kLater;
+  const int at = atomicAdd(a.left, 1);
+  if (at < kMaxLeft) a.left[kLeftRows + at] = s;
+}
+
 // What a kernel serves: rows that a list or the warps' sums can tell, the others are left; all; those that were left.
 enum Mode { kEasy, kAll, kLeft };
 
@@ -341,7 +348,7 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
       if (!exact) {
         const Found f = row.draw_all(u_last, total, taken, out);
         if constexpr (kMode == kEasy) {
-          if (f.mine && f.close) a.token[s] = kLater;
+          if (f.mine && f.close) leave(a, s);
           else write(f, total);
         } else {
           Mail m{};
@@ -374,8 +381,10 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
     }
     for (int j = len + tid; j < a.D; j += kThreads) a.path_node[static_cast<int64_t>(s) * a.D + j] = -1;
     for (int j = len + 1 + tid; j <= a.D; j += kThreads) a.token[static_cast<int64_t>(s) * (a.D + 1) + j] = -1;
+  } else if (tid == 0 && later) {
+    leave(a, s);
   } else if (tid == 0 && !drawn) {
-    a.token[s] = later ? kLater : last;
+    a.token[s] = last;
     if (a.logp) a.logp[s] = 0.f;
     if (a.n_kept) a.n_kept[s] = last < 0 ? 0 : 1;
   }
@@ -398,22 +407,29 @@ __global__ void __launch_bounds__(kClusterThreads, 2) limited_kernel(LimitedArgs
   serve<T, kCluster, kClusterThreads, kTree, kAll>(a, sh, static_cast<int>(blockIdx.x / kCluster), static_cast<int>(blockIdx.x % kCluster));
 }
 
-// The rows that many_rows_kernel has left, those of a cluster a fixed share of all.
+// The rows that many_rows_kernel has left.
 template <typename T, int kCluster>
 __global__ void __launch_bounds__(kClusterThreads, 2) left_rows_kernel(LimitedArgs a) {
   __shared__ Shared<kCluster, kClusterThreads, true> sh;
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int rank = static_cast<int>(blockIdx.x % kCluster), clusters = static_cast<int>(gridDim.x / kCluster);
-  const int lane = threadIdx.x & 31;
-  for (int64_t s0 = blockIdx.x / kCluster; s0 < a.N; s0 += 32ll * clusters) {
-    // (a row's mark is only changed by its own cluster, behind a barrier of all its CTAs)
-    const int64_t mine = s0 + static_cast<int64_t>(lane) * clusters;
-    unsigned left = __ballot_sync(kFull, mine < a.N && a.token[mine < a.N ? mine : 0] == kLater);
-    while (left) {
-      const int at = __ffs(left) - 1;
-      left &= left - 1;
-      serve<T, kCluster, kClusterThreads, false, kLeft>(a, sh, static_cast<int>(s0 + static_cast<int64_t>(at) * clusters), rank);
-    }
+  const int left = a.left[0];
+  if (left <= kMaxLeft) {
+    for (int i = blockIdx.x / kCluster; i < left; i += clusters)
+      serve<T, kCluster, kClusterThreads, false, kLeft>(a, sh, a.left[kLeftRows + i], rank);
+  }
+  // the last one to have read the count sets it to 0 for the next call
+  if (threadIdx.x == 0) {
+    __threadfence();
+    if (atomicAdd(a.left + 1, 1) == static_cast<int>(gridDim.x) - 1) a.left[0] = a.left[1] = 0;
+  }
+  if (left <= kMaxLeft) return;
+  // (more than the list holds: every cluster looks at its share of the rows.  A row's mark is only changed by its own
+  // cluster, behind a barrier of all its CTAs)
+  for (int64_t s = blockIdx.x / kCluster; s < a.N; s += clusters) {
+    const bool mine = a.token[s] == kLater;
+    if (kCluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+    if (mine) serve<T, kCluster, kClusterThreads, false, kLeft>(a, sh, static_cast<int>(s), rank);
   }
 }
 
