@@ -51,25 +51,24 @@ size_t layout(int64_t S, int64_t max_pages, int64_t n_pages, char* p, Workspace*
   return at;
 }
 
-// Sum of v over the threads before this one; *all receives the sum over all.  s_warp: 33 ints.
+// Sum of v over the threads before this one; *all receives the sum over all.  s_warp: 32 ints.
 __device__ __forceinline__ int scan_before(int v, int* s_warp, int* all) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  int upto = v;
+  const auto scan = [&](int x) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int y = __shfl_up_sync(kFull, upto, o);
-    if (lane >= o) upto += y;
-  }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int y = __shfl_up_sync(kFull, x, o);
+      if (lane >= o) x += y;
+    }
+    return x;
+  };
+  const int upto = scan(v);
   __syncthreads();  // (s_warp may still be read from the last call)
   if (lane == 31) s_warp[warp] = upto;
   __syncthreads();
-  int before = 0, sum = 0;
-  for (int w = 0; w < kPlanThreads / 32; ++w) {
-    if (w == warp) before = sum;
-    sum += s_warp[w];
-  }
-  *all = sum;
-  return before + upto - v;
+  const int warps = scan(s_warp[lane]);  // every warp for itself
+  *all = __shfl_sync(kFull, warps, 31);
+  return __shfl_sync(kFull, warps, warp) - s_warp[warp] + upto - v;
 }
 
 __device__ __forceinline__ bool is_page(const PoolArgs& p, int page) { return page >= 0 && page < p.n_pages; }
@@ -81,8 +80,13 @@ __device__ __forceinline__ bool fits(const PoolArgs& p, int held, int len) {
   return held >= 0 && held <= p.max_pages && len >= 0 && len <= static_cast<int64_t>(held) * p.page_size;
 }
 
+// A plan lets its execution get ready, which waits for it.
+__device__ __forceinline__ void plan_begins() { asm volatile("griddepcontrol.launch_dependents;" ::: "memory"); }
+__device__ __forceinline__ void wait_for_plan() { asm volatile("griddepcontrol.wait;" ::: "memory"); }
+
 // ---- fork
 __global__ void __launch_bounds__(kThreads) fork_plan_kernel(PoolArgs p, const int32_t* parent, Workspace w) {
+  plan_begins();
   const int s = blockIdx.x, tid = threadIdx.x;
   const int from = parent[s];
   const int held = p.held[s];
@@ -99,21 +103,38 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(PoolArgs p, const i
       }
     }
     const int32_t* row = p.page_table + static_cast<int64_t>(from < 0 ? 0 : from) * p.max_pages;
-    if (!bad)
-      for (int j = tid; j < need; j += kThreads) bad |= !is_page(p, row[j]);
+    const int32_t* own = p.page_table + static_cast<int64_t>(s) * p.max_pages;
+    constexpr int kKeep = 4;  // of each row's pages a thread reads these at once
+    int page[kKeep], old[kKeep];
+    if (bad) need = 0;
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) {
+      const int j = tid + i * kThreads;
+      page[i] = j < need ? row[j] : -1;
+      old[i] = !bad && j < held ? own[j] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < kKeep; ++i) bad |= tid + i * kThreads < need && !is_page(p, page[i]);
+    for (int j = tid + kKeep * kThreads; j < need; j += kThreads) bad |= !is_page(p, row[j]);
     bad = __syncthreads_or(bad);
     if (!bad) {
       bool odd = false;
-      for (int j = tid; j < need; j += kThreads) {
-        const int page = row[j];
-        w.rows[static_cast<int64_t>(s) * p.max_pages + j] = page;
-        atomicAdd(p.ref_count + page, 1);
-      }
-      for (int j = tid; j < held; j += kThreads) {
-        const int page = p.page_table[static_cast<int64_t>(s) * p.max_pages + j];
-        if (is_page(p, page)) atomicSub(p.ref_count + page, 1);
+      const auto take = [&](int j, int q) {
+        w.rows[static_cast<int64_t>(s) * p.max_pages + j] = q;
+        atomicAdd(p.ref_count + q, 1);
+      };
+      const auto drop = [&](int q) {
+        if (is_page(p, q)) atomicSub(p.ref_count + q, 1);
         else odd = true;
+      };
+#pragma unroll
+      for (int i = 0; i < kKeep; ++i) {
+        const int j = tid + i * kThreads;
+        if (j < need) take(j, page[i]);
+        if (j < held) drop(old[i]);
       }
+      for (int j = tid + kKeep * kThreads; j < need; j += kThreads) take(j, row[j]);
+      for (int j = tid + kKeep * kThreads; j < held; j += kThreads) drop(own[j]);
       if (odd) atomicOr(p.status, kStatusBadIndex);
     }
   }
@@ -124,6 +145,7 @@ __global__ void __launch_bounds__(kThreads) fork_plan_kernel(PoolArgs p, const i
 }
 
 __global__ void __launch_bounds__(kThreads) fork_apply_kernel(PoolArgs p, Workspace w) {
+  wait_for_plan();
   const int s = blockIdx.x;
   const Plan plan = w.plan[s];
   if (plan.need < 0) return;
@@ -138,6 +160,7 @@ __global__ void __launch_bounds__(kThreads) fork_apply_kernel(PoolArgs p, Worksp
 // ---- resize
 __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(PoolArgs p, const int32_t* want, Workspace w) {
   __shared__ int s_warp[kPlanThreads / 32];
+  plan_begins();
   const int tid = threadIdx.x;
   // Whether slot j of a sequence, which will be written, is named elsewhere too.
   const auto shared_slot = [&](int s, int j, bool* bad) {
@@ -148,7 +171,7 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(PoolArgs p, c
     }
     return p.ref_count[page] > 1;
   };
-  int total = 0;
+  int total = 0, any_swaps = 0;
   for (int s0 = 0; s0 < p.S; s0 += kPlanThreads) {
     const int s = s0 + tid;
     Plan plan{-1, 0, 0, 0};
@@ -176,15 +199,24 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(PoolArgs p, c
     plan.base = total + scan_before(fresh, s_warp, &sum);
     total += sum;
     if (s < p.S) w.plan[s] = plan;
+    any_swaps |= plan.swaps > 0;
   }
-  // the lowest free pages, as many as are needed
+  any_swaps = __syncthreads_or(any_swaps);
+  // the lowest free pages, as many as are needed (a thread looks at kLook neighbours at a time)
+  constexpr int kLook = 4;
   int found = 0;
-  for (int p0 = 0; p0 < p.n_pages && found < total; p0 += kPlanThreads) {
-    const int page = p0 + tid;
-    const bool is_free = page < p.n_pages && p.ref_count[page] == 0;
+  for (int p0 = 0; p0 < p.n_pages && found < total; p0 += kLook * kPlanThreads) {
+    const int first = p0 + kLook * tid;
+    int count[kLook], n = 0;
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) count[i] = first + i < p.n_pages ? p.ref_count[first + i] : 1;
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) n += count[i] == 0;
     int sum;
-    const int at = found + scan_before(is_free, s_warp, &sum);
-    if (is_free && at < total) w.list[at] = page;
+    int at = found + scan_before(n, s_warp, &sum);
+#pragma unroll
+    for (int i = 0; i < kLook; ++i)
+      if (count[i] == 0 && at < total) w.list[at++] = first + i;
     found += sum;
   }
   __syncthreads();
@@ -213,6 +245,7 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(PoolArgs p, c
         }
       }
     }
+    if (!any_swaps) continue;
     int sum;
     const int at = n_copies + scan_before(copy.entries > 0, s_warp, &sum);
     if (copy.entries > 0) w.copies[at] = copy;
@@ -221,43 +254,73 @@ __global__ void __launch_bounds__(kPlanThreads) resize_plan_kernel(PoolArgs p, c
   if (tid == 0) w.counts[0] = n_copies;
 }
 
-// 16-byte vectors of `entries` entries of a page, keys or values of one layer, from one page to another.
-__device__ __forceinline__ void copy_entries(const CacheArgs& c, bool key, int layer, int src, int dst, int entries) {
-  const int64_t page = key ? c.k_page : c.v_page, entry = key ? c.k_entry : c.v_entry, head = key ? c.k_head : c.v_head;
-  char* base = (key ? c.k : c.v) + layer * (key ? c.k_layer : c.v_layer);
-  const char* from = base + src * page;
-  char* to = base + dst * page;
-  const int per_head = c.head_dim * (c.dtype == GTO_F32 ? 4 : 2) / 16;
-  const int cols = c.n_kv_heads * per_head;
-  const int64_t n = static_cast<int64_t>(entries) * cols;
-  constexpr int kBatch = 8;
-  for (int64_t i0 = threadIdx.x; i0 < n; i0 += kBatch * kThreads) {
-    uint4 x[kBatch];
-    int64_t at[kBatch];
+// ---- copies of pages: units of kUnit bytes of the keys or the values of one layer, eight loads of 16 bytes a thread on their
+// way at a time.
+constexpr int kAtOnce = 8;
+constexpr int kUnit = kAtOnce * kThreads;  // vectors
+constexpr int kCopyBlocks = 6;             // CTAs an SM
+
+struct Units {
+  int cols;           // vectors of an entry: heads one after the other
+  int per_head;       // vectors of a head
+  int chunks;         // units of a page
+  bool k_dense, v_dense;  // whether the entries of a page lie without gaps
+};
+
+// f(i, &from, &to, &entries): the i-th copy of n.
+template <typename F>
+__device__ __forceinline__ void copy_pages(const CacheArgs& c, const Units& u, int n, int block, int blocks, F f) {
+  const int64_t parts = 2ll * c.n_layers * u.chunks, units = n * parts;
+  for (int64_t unit = block; unit < units; unit += blocks) {
+    const int copy = static_cast<int>(unit / parts);
+    const uint32_t part = static_cast<uint32_t>(unit - copy * parts);
+    const int layer = static_cast<int>(part / u.chunks >> 1), chunk = static_cast<int>(part % u.chunks);
+    const bool key = part / u.chunks & 1;
+    int src, dst, entries;
+    f(copy, &src, &dst, &entries);
+    const int64_t page = key ? c.k_page : c.v_page;
+    char* base = (key ? c.k : c.v) + layer * (key ? c.k_layer : c.v_layer);
+    const char* from = base + src * page;
+    char* to = base + dst * page;
+    const int64_t size = static_cast<int64_t>(entries) * u.cols;
+    const int64_t first = static_cast<int64_t>(chunk) * kUnit + threadIdx.x;
+    if (first - threadIdx.x >= size) continue;
+    uint4 x[kAtOnce];
+    if (key ? u.k_dense : u.v_dense) {
 #pragma unroll
-    for (int b = 0; b < kBatch; ++b) {
-      const int64_t i = i0 + b * kThreads;
-      if (i < n) {
-        const int e = static_cast<int>(i / cols), col = static_cast<int>(i % cols);
-        at[b] = e * entry + (col / per_head) * head + (col % per_head) * 16;
-        x[b] = *reinterpret_cast<const uint4*>(from + at[b]);
-      }
+      for (int b = 0; b < kAtOnce; ++b)
+        if (first + b * kThreads < size) x[b] = ld_stream16(from + (first + b * kThreads) * 16);
+#pragma unroll
+      for (int b = 0; b < kAtOnce; ++b)
+        if (first + b * kThreads < size) st_stream16(to + (first + b * kThreads) * 16, x[b]);
+    } else {
+      const int64_t entry = key ? c.k_entry : c.v_entry, head = key ? c.k_head : c.v_head;
+      const auto place = [&](int b) {
+        const int64_t i = first + b * kThreads;
+        const int64_t e = i / u.cols;
+        const uint32_t col = static_cast<uint32_t>(i - e * u.cols);
+        return e * entry + (col / u.per_head) * head + (col % u.per_head) * 16;
+      };
+#pragma unroll
+      for (int b = 0; b < kAtOnce; ++b)
+        if (first + b * kThreads < size) x[b] = ld_stream16(from + place(b));
+#pragma unroll
+      for (int b = 0; b < kAtOnce; ++b)
+        if (first + b * kThreads < size) st_stream16(to + place(b), x[b]);
     }
-#pragma unroll
-    for (int b = 0; b < kBatch; ++b)
-      if (i0 + b * kThreads < n) *reinterpret_cast<uint4*>(to + at[b]) = x[b];
   }
 }
 
 // Block s < S: the tables of sequence s; the others: the copies.
-__global__ void __launch_bounds__(kThreads) resize_apply_kernel(PoolArgs p, CacheArgs c, Workspace w) {
+__global__ void __launch_bounds__(kThreads) resize_apply_kernel(PoolArgs p, CacheArgs c, Units u, Workspace w) {
+  wait_for_plan();
   if (static_cast<int>(blockIdx.x) >= p.S) {
-    const int n = w.counts[0], units = 2 * c.n_layers;
-    for (int64_t i = blockIdx.x - p.S; i < static_cast<int64_t>(n) * units; i += gridDim.x - p.S) {
-      const Copy copy = w.copies[i / units];
-      const int u = static_cast<int>(i % units);
-      copy_entries(c, u & 1, u >> 1, copy.src, copy.dst, copy.entries);
-    }
+    copy_pages(c, u, w.counts[0], blockIdx.x - p.S, gridDim.x - p.S, [&](int i, int* src, int* dst, int* entries) {
+      const Copy copy = w.copies[i];
+      *src = copy.src;
+      *dst = copy.dst;
+      *entries = copy.entries;
+    });
     return;
   }
   const int s = blockIdx.x, tid = threadIdx.x;
@@ -295,28 +358,40 @@ __global__ void __launch_bounds__(kThreads) resize_apply_kernel(PoolArgs p, Cach
 // ---- compact
 __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PoolArgs p, int32_t* ref_out, int32_t* n_used, Workspace w) {
   __shared__ int s_warp[kPlanThreads / 32];
+  plan_begins();
   const int tid = threadIdx.x;
   int used = 0;
+#pragma unroll 8
   for (int page = tid; page < p.n_pages; page += kPlanThreads) used += p.ref_count[page] > 0;
   int total;
   scan_before(used, s_warp, &total);
   int holes = 0, movers = 0;
   int32_t* hole = w.to + p.n_pages;
-  for (int p0 = 0; p0 < p.n_pages; p0 += kPlanThreads) {
-    const int page = p0 + tid;
-    const bool in = page < p.n_pages;
-    const bool is_used = in && p.ref_count[page] > 0;
-    const bool is_hole = in && !is_used && page < total, moves = is_used && page >= total;
+  constexpr int kLook = 4;
+  for (int p0 = 0; p0 < p.n_pages; p0 += kLook * kPlanThreads) {
+    const int first = p0 + kLook * tid;
+    int count[kLook], n = 0;  // holes below, movers from `total` on: never both at one page
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) count[i] = first + i < p.n_pages ? p.ref_count[first + i] : 0;
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) {
+      const int page = first + i;
+      if (page < p.n_pages) n += page < total ? count[i] <= 0 : (count[i] > 0) << 16;
+    }
     int sum;
-    const int at_hole = holes + scan_before(is_hole, s_warp, &sum);
-    holes += sum;
-    const int at_move = movers + scan_before(moves, s_warp, &sum);
-    movers += sum;
-    if (is_hole) hole[at_hole] = page;
-    if (moves) w.list[at_move] = page;
-    if (in) {
+    const int before = scan_before(n, s_warp, &sum);  // (4096 pages a turn: neither half overflows)
+    int at_hole = holes + (before & 0xffff), at_move = movers + (before >> 16);
+    holes += sum & 0xffff;
+    movers += sum >> 16;
+#pragma unroll
+    for (int i = 0; i < kLook; ++i) {
+      const int page = first + i;
+      if (page >= p.n_pages) continue;
+      const bool is_used = count[i] > 0;
+      if (!is_used && page < total) hole[at_hole++] = page;
+      if (is_used && page >= total) w.list[at_move++] = page;
       w.to[page] = page;
-      ref_out[page] = is_used && !moves ? p.ref_count[page] : 0;
+      ref_out[page] = is_used && page < total ? count[i] : 0;
     }
   }
   __syncthreads();
@@ -332,13 +407,14 @@ __global__ void __launch_bounds__(kPlanThreads) compact_plan_kernel(PoolArgs p, 
 }
 
 // Block s < S: the table of sequence s; the others: the pages that move.
-__global__ void __launch_bounds__(kThreads) compact_apply_kernel(PoolArgs p, CacheArgs c, int32_t* table_out, Workspace w) {
+__global__ void __launch_bounds__(kThreads) compact_apply_kernel(PoolArgs p, CacheArgs c, Units u, int32_t* table_out, Workspace w) {
+  wait_for_plan();
   if (static_cast<int>(blockIdx.x) >= p.S) {
-    const int n = w.counts[0], units = 2 * c.n_layers;
-    for (int64_t i = blockIdx.x - p.S; i < static_cast<int64_t>(n) * units; i += gridDim.x - p.S) {
-      const int page = w.list[i / units], u = static_cast<int>(i % units);
-      copy_entries(c, u & 1, u >> 1, page, w.to[page], p.page_size);
-    }
+    copy_pages(c, u, w.counts[0], blockIdx.x - p.S, gridDim.x - p.S, [&](int i, int* src, int* dst, int* entries) {
+      *src = w.list[i];
+      *dst = w.to[*src];
+      *entries = p.page_size;
+    });
     return;
   }
   const int s = blockIdx.x, held = p.held[s];
@@ -353,10 +429,39 @@ __global__ void __launch_bounds__(kThreads) compact_apply_kernel(PoolArgs p, Cac
   if (bad) atomicOr(p.status, kStatusBadIndex);
 }
 
-Workspace workspace_of(const PoolArgs& p, int S, void* ws) {
+Workspace workspace_of(const PoolArgs& p, void* ws) {
   Workspace w;
-  layout(S, p.max_pages, p.n_pages, static_cast<char*>(ws), &w);
+  layout(p.S, p.max_pages, p.n_pages, static_cast<char*>(ws), &w);
   return w;
+}
+
+Units units_of(const PoolArgs& p, const CacheArgs& c) {
+  Units u;
+  const int e = c.dtype == GTO_F32 ? 4 : 2, head = c.head_dim * e;
+  u.per_head = head / 16;
+  u.cols = c.n_kv_heads * u.per_head;
+  u.chunks = static_cast<int>((static_cast<int64_t>(p.page_size) * u.cols + kUnit - 1) / kUnit);
+  const auto dense = [&](int64_t entry, int64_t h) {
+    return (c.n_kv_heads == 1 || h == head) && (p.page_size == 1 || entry == static_cast<int64_t>(c.n_kv_heads) * head);
+  };
+  u.k_dense = dense(c.k_entry, c.k_head);
+  u.v_dense = dense(c.v_entry, c.v_head);
+  return u;
+}
+
+// The execution of a plan.
+template <typename... P, typename... A>
+cudaError_t after_plan(void (*kernel)(P...), int blocks, cudaStream_t stream, A... args) {
+  cudaLaunchConfig_t cfg{};
+  cfg.gridDim = dim3(static_cast<unsigned>(blocks));
+  cfg.blockDim = dim3(kThreads);
+  cfg.stream = stream;
+  cudaLaunchAttribute attr{};
+  attr.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  attr.val.programmaticStreamSerializationAllowed = 1;
+  cfg.attrs = &attr;
+  cfg.numAttrs = 1;
+  return cudaLaunchKernelEx(&cfg, kernel, args...);
 }
 
 }  // namespace
@@ -364,29 +469,29 @@ Workspace workspace_of(const PoolArgs& p, int S, void* ws) {
 size_t pages_workspace(const gto_decode_config& c) { return layout(c.S, c.max_pages, c.n_pages, nullptr, nullptr); }
 
 cudaError_t launch_pages_fork(const PoolArgs& p, const int32_t* parent, void* ws, cudaStream_t stream, int64_t* launches) {
-  const Workspace w = workspace_of(p, p.S, ws);
+  const Workspace w = workspace_of(p, ws);
   *launches += 2;
   fork_plan_kernel<<<p.S, kThreads, 0, stream>>>(p, parent, w);
-  fork_apply_kernel<<<p.S, kThreads, 0, stream>>>(p, w);
-  return cudaGetLastError();
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : after_plan(fork_apply_kernel, p.S, stream, p, w);
 }
 
 cudaError_t launch_pages_resize(const PoolArgs& p, const int32_t* want, const CacheArgs& c, void* ws, int sms,
                                 cudaStream_t stream, int64_t* launches) {
-  const Workspace w = workspace_of(p, p.S, ws);
+  const Workspace w = workspace_of(p, ws);
   *launches += 2;
   resize_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p, want, w);
-  resize_apply_kernel<<<p.S + 8 * sms, kThreads, 0, stream>>>(p, c, w);
-  return cudaGetLastError();
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : after_plan(resize_apply_kernel, p.S + kCopyBlocks * sms, stream, p, c, units_of(p, c), w);
 }
 
 cudaError_t launch_pages_compact(const PoolArgs& p, const CacheArgs& c, int32_t* table_out, int32_t* ref_out, int32_t* n_used,
                                  void* ws, int sms, cudaStream_t stream, int64_t* launches) {
-  const Workspace w = workspace_of(p, p.S, ws);
+  const Workspace w = workspace_of(p, ws);
   *launches += 2;
   compact_plan_kernel<<<1, kPlanThreads, 0, stream>>>(p, ref_out, n_used, w);
-  compact_apply_kernel<<<p.S + 8 * sms, kThreads, 0, stream>>>(p, c, table_out, w);
-  return cudaGetLastError();
+  const cudaError_t e = cudaGetLastError();
+  return e != cudaSuccess ? e : after_plan(compact_apply_kernel, p.S + kCopyBlocks * sms, stream, p, c, units_of(p, c), table_out, w);
 }
 
 }  // namespace gto
