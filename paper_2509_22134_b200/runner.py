@@ -101,7 +101,8 @@ class DecodeStep:
 
     A step is begin(), attend() for every layer, verify() and commit(), all on the current stream; nothing
     waits for the device, and a step can be captured into a CUDA graph.  kv_len holds the cached entries of
-    every sequence; page_table is the caller's to fill (a page may be added between steps).
+    every sequence; page_table is the caller's to fill (a page may be added between steps), or, where cfg has
+    GTO_DECODE_PAGES, reserve(), fork() and compact() manage it (the caller then leaves it alone).
     """
 
     def __init__(self, cfg: gto.gto_decode_config, n_layers: int, inv_freq, device="cuda:0"):
@@ -117,6 +118,14 @@ class DecodeStep:
         self.kv_len = torch.zeros(cfg.S, dtype=torch.int32, device=self.device)
         self.inv_freq = torch.as_tensor(inv_freq, dtype=torch.float64, device=self.device)
         self.verdict = gto.alloc_verdict(cfg, self.device)
+        self.drawn = {"token": torch.zeros(cfg.S, dtype=torch.int32, device=self.device),
+                      "logp": torch.zeros(cfg.S, dtype=torch.float32, device=self.device),
+                      "n_kept": torch.zeros(cfg.S, dtype=torch.int32, device=self.device)}
+        self.pool = None
+        if cfg.flags & gto.GTO_DECODE_PAGES:
+            self.pool = dict(gto.alloc_page_pool(cfg, self.device), page_table=self.page_table, kv_len=self.kv_len)
+            self.moved = (torch.empty_like(self.page_table), torch.empty_like(self.pool["ref_count"]),
+                          torch.zeros(1, dtype=torch.int32, device=self.device))
         self.q_rotated = torch.empty((cfg.T, cfg.n_q_heads, cfg.head_dim), dtype=dtype, device=self.device)
         self.batch = None
         self.tokens = None  # rows that this step's layers were given, the fewest
@@ -142,9 +151,39 @@ class DecodeStep:
                           self.inv_freq, q_norm, k_norm)
         gto.gto_tree_attention(self.ctx, self.batch, rotated, self.k_cache[layer], self.v_cache[layer], out, lse)
 
-    def verify(self, trees: dict, target, d2t, temperature, u_node, u_bonus) -> dict:
-        gto.gto_verify_tree(self.ctx, trees, target, d2t, temperature, u_node, u_bonus, self.verdict)
+    def verify(self, trees: dict, target, d2t, temperature, u_node, u_bonus, limits: dict | None = None) -> dict:
+        """limits: any of top_k, top_p and min_p, for every sequence."""
+        if limits:
+            gto.gto_verify_tree_limited(self.ctx, trees, target, d2t, dict(limits, temperature=temperature), u_node, u_bonus,
+                                        self.verdict)
+        else:
+            gto.gto_verify_tree(self.ctx, trees, target, d2t, temperature, u_node, u_bonus, self.verdict)
         return self.verdict
+
+    def sample(self, logits, temperature, u, limits: dict | None = None, rows=None) -> dict:
+        """A token for each of N sequences from logits [n_rows, V_target] (a prompt's last rows; n draws from one row with
+        `rows`), with its log-probability and the number of tokens it was drawn from: views that the next call overwrites."""
+        out = {n: t[:temperature.numel()] for n, t in self.drawn.items()}
+        gto.gto_sample_tokens(self.ctx, logits, dict(limits or {}, temperature=temperature), u, out["token"], logp=out["logp"],
+                              n_kept=out["n_kept"], rows=rows)
+        return out
+
+    def reserve(self, want):
+        """Pages for want [S] entries (negative: as it is; fewer than it has: the rest goes back), in all layers; the page that
+        the next entries go into is the sequence's own afterwards."""
+        gto.gto_pages_resize(self.ctx, self.pool, want, self.k_cache, self.v_cache)
+
+    def fork(self, parent):
+        """Sequence s continues what parent[s] has (itself: as it is; -1: it ends, and its pages go back)."""
+        gto.gto_pages_fork(self.ctx, self.pool, parent)
+
+    def compact(self):
+        """The pages in use move to the front of the cache; the number of them, on the device."""
+        table, ref, used = self.moved
+        gto.gto_pages_compact(self.ctx, self.pool, self.k_cache, self.v_cache, table, ref, used)
+        self.page_table.copy_(table)
+        self.pool["ref_count"].copy_(ref)
+        return used
 
     def commit(self):
         """Keeps the accepted nodes' entries in all layers; kv_len then counts them.  A sequence that the other calls
