@@ -11,11 +11,11 @@ constexpr int kBins = 128;              // of the slots' maxima, by their distan
 constexpr int kWideBins = 2048;         // of the tokens, where more stays than a list holds
 
 // How far a sum of fp32 weights can be from the true one, relative to the row's whole mass.  A weight 2^-a is off by
-// 2^-22 (the exponential) and 2^-24 a ln 2 (rounding of z - ref; the rest of the argument is carried in two words)
-// relative to itself, and the mean of a over the distribution is at most log2 V <= 19.6; kReach more where the reference lags;
-// 32 weights of a thread and 32 threads are added in fp32, in ten levels (10 * 2^-24), the rest in fp64.  In all below 1.9e-6.
+// 2^-22 (the exponential) and 3 * 2^-24 * (a + kReach) * ln 2 (roundings of its argument) relative to itself; the mean of a
+// over the distribution is at most log2 V <= 19.6; a thread's 32 weights and those of 32 threads are added in fp32, in twelve
+// levels (12 * 2^-24), the rest in fp64.  In all below 3.9e-6.  (The argument in two words halved that and took half as long again.)
 constexpr float kReach = 4.f;
-constexpr double kSlack = 2e-6;
+constexpr double kSlack = 4e-6;
 
 // ---- shared memory of the CTAs of a cluster
 __device__ __forceinline__ uint64_t far_u64(const void* p, int cta) {
@@ -48,51 +48,6 @@ __device__ __forceinline__ N sum_warp(N v) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v += __shfl_xor_sync(kFull, v, o);
   return v;
-}
-
-// The scale of the weights in two words; and the distance from which on a weight is 0 (further ones count as that far, so
-// that the product's remainder is a number).
-struct Scale {
-  float hi, lo, far;
-};
-// 2^(d c): the product's rounding and the low word come in by the first term of the series.
-__device__ __forceinline__ float fine_weight(float d, const Scale& c) {
-  d = fmaxf(d, c.far);
-  const float x = d * c.hi;
-  const float w = ex2_approx(x);
-  return fmaf(w, fmaf(d, c.lo, fmaf(d, c.hi, -x)) * 0.69314718f, w);
-}
-// Sum of the weights of 16 bytes of logits, 2^((f - m) c), in fp32: pairs side by side.
-template <typename T>
-__device__ __forceinline__ float fine_weights(const uint4& v, float m, const Scale& c) {
-  constexpr int E = T::kPerVec;
-  float f[E];
-  T::unpack(v, f);
-  uint64_t hi, lo, ln2, sum[E / 2];
-  asm("mov.b64 %0, {%1, %1};" : "=l"(hi) : "f"(c.hi));
-  asm("mov.b64 %0, {%1, %1};" : "=l"(lo) : "f"(c.lo));
-  asm("mov.b64 %0, {%1, %1};" : "=l"(ln2) : "f"(0.69314718f));
-#pragma unroll
-  for (int e = 0; e < E / 2; ++e) {
-    float a, b;
-    uint64_t d, x, w, r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(d) : "f"(fmaxf(f[2 * e] - m, c.far)), "f"(fmaxf(f[2 * e + 1] - m, c.far)));
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(x) : "l"(d), "l"(hi));
-    asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(x));
-    asm("mov.b64 %0, {%1, %2};" : "=l"(w) : "f"(ex2_approx(a)), "f"(ex2_approx(b)));
-    asm("mov.b64 %0, {%1, %2};" : "=l"(x) : "f"(-a), "f"(-b));
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(d), "l"(hi), "l"(x));
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(d), "l"(lo), "l"(r));
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(r), "l"(ln2));
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(sum[e]) : "l"(w), "l"(r), "l"(w));
-  }
-#pragma unroll
-  for (int w = E / 4; w > 0; w /= 2)
-#pragma unroll
-    for (int e = 0; e < w; ++e) asm("add.rn.f32x2 %0, %1, %2;" : "=l"(sum[e]) : "l"(sum[e]), "l"(sum[e + w]));
-  float a, b;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(sum[0]));
-  return a + b;
 }
 
 // The next bf16 at or above x, as its bits.
@@ -170,7 +125,8 @@ struct Row {
   static constexpr int kWarps = Mem::kWarps;
   static constexpr int E = T::kPerVec;
   static constexpr int kSlots = Mem::kSlots, kList = Mem::kList, kMaxSteps = Mem::kMaxSteps, kItems = Mem::kItems;
-  static constexpr int kAim = kList * 5 / 6;  // tokens that a list is made for
+  // tokens that a list is made for (where many rows share an SM, only so many that a thread sorts one each)
+  static constexpr int kAim = kServesAll ? kList * 5 / 6 : 240;
   static constexpr int kEach = kList / kThreads;
   static constexpr int kMails = kCluster * kWarps;
   static constexpr int kMailRounds = (kMails + 31) / 32;
@@ -181,7 +137,7 @@ struct Row {
   int turn, flip;  // of the double-buffered exchanges between CTAs / warps
   float M;         // the row's largest logit
   double scale;    // to log2 units
-  Scale c;
+  float c2;        // the same in fp32
 
   __device__ __forceinline__ Row(Mem& shared, int V, int r) : sh(shared) {
     rank = r;
@@ -199,9 +155,7 @@ struct Row {
   }
   __device__ __forceinline__ void scale_to(double s) {
     scale = s;
-    c.hi = static_cast<float>(s);
-    c.lo = static_cast<float>(s - static_cast<double>(c.hi));
-    c.far = -1e30f / c.hi;
+    c2 = static_cast<float>(s);
   }
   __device__ __forceinline__ void cluster_sync() const {
     if (kCluster == 1) __syncthreads();
@@ -363,7 +317,7 @@ struct Row {
   // masked: whether to look for -inf; then whether there is one.
   template <bool kSum>
   __device__ __forceinline__ bool stream(double* mass, bool* masked) {
-    const float reach = kReach / c.hi;
+    const float reach = kReach / c2;
     float ref = -INFINITY, most = -INFINITY, slot_top = -INFINITY;
     bool bad = false, low = false;
     int slot = 0, in_slot = 0;
@@ -403,7 +357,7 @@ struct Row {
         float s = 0.f;
         if (ref != -INFINITY) {
 #pragma unroll
-          for (int u = 0; u < kUnroll; ++u) s += fine_weights<T>(v[u], ref, c);
+          for (int u = 0; u < kUnroll; ++u) s += weights<T>(v[u], ref, c2);
         }
         s = warp_sum_f32(s);
         if (lane == 0) sh.part[step][warp] = Part{s, ref};
@@ -962,9 +916,9 @@ struct Row {
           T::unpack(v[q], x);
 #pragma unroll
           for (int e = 0; e < E; ++e)
-            if (!out(i * E + e)) w[q] += static_cast<double>(fine_weight(x[e] - M, c));
+            if (!out(i * E + e)) w[q] += static_cast<double>(ex2_approx((x[e] - M) * c2));
         } else {
-          w[q] = static_cast<double>(fine_weights<T>(v[q], M, c));
+          w[q] = static_cast<double>(weights<T>(v[q], M, c2));
         }
       }
       upto[q] = scan_warp(w[q], lane);
@@ -1006,7 +960,7 @@ struct Row {
 #pragma unroll
     for (int e = 0; e < E; ++e) {
       const int id = i * E + e;
-      const double y = out(id) ? 0.0 : static_cast<double>(fine_weight(x[e] - M, c));
+      const double y = out(id) ? 0.0 : static_cast<double>(ex2_approx((x[e] - M) * c2));
       if (f.id < 0 && y > 0.0 && acc + y > aim) {
         f.id = id;
         found = x[e];
@@ -1041,18 +995,21 @@ struct Row {
 #pragma unroll
     for (int e = 0; e < E; ++e) w[e] = x[e] >= from ? w[e] : 0.0;
   }
+  static __device__ __forceinline__ double sum_of(const double (&w)[E]) {
+    if (E == 4) return (w[0] + w[1]) + (w[2] + w[3]);
+    return ((w[0] + w[1]) + (w[2] + w[3])) + ((w[E - 4] + w[E - 3]) + (w[E - 2] + w[E - 1]));
+  }
   // The row's mass in fp64.
   __device__ __forceinline__ double whole() {
-    double m[2] = {0.0, 0.0};
+    double m = 0.0;
     const float from = near_from();
     vectors([&](const uint4& v, int) {
       float x[E];
       double w[E];
       raw_of(v, from, x, w);
-#pragma unroll
-      for (int e = 0; e < E; ++e) m[e & 1] += w[e];
+      m += sum_of(w);
     });
-    return reduce(m[0] + m[1], 0.0, 0, 0).a;
+    return reduce(m, 0.0, 0, 0).a;
   }
   // Of the runs' masses `mine`: the first id at which the cumulative sum of weight(value, id) passes u * (the whole sum),
   // or `aim` where u < 0.  Found in one lane of the cluster; id -1 where nothing has a weight.
@@ -1117,16 +1074,15 @@ struct Row {
 
   // The token of a row of which all stays, in fp64.
   __device__ __forceinline__ Found locate_all(double u) {
-    double m[2] = {0.0, 0.0};
+    double m = 0.0;
     const float from = near_from();
     along([&](const uint4& v, int) {
       float x[E];
       double w[E];
       raw_of(v, from, x, w);
-#pragma unroll
-      for (int e = 0; e < E; ++e) m[e & 1] += w[e];
+      m += sum_of(w);
     });
-    return pick(m[0] + m[1], [&](float x, int) { return raw(x); }, u, 0.0);
+    return pick(m, [&](float x, int) { return raw(x); }, u, 0.0);
   }
 
   // ---- rows of which more stays than a list holds: the tokens are counted by their distance from the largest logit, which
@@ -1249,153 +1205,171 @@ struct Row {
       if (edge & 1) b0 = max(b - 1, 0);
       if (edge & 2) b1 = min(b + 1, kWideBins - 2);
     }
-    uint32_t lo, hi, lo2 = 0xffffffffu, hi2 = orderable(-INFINITY);  // (the second one holds nothing)
-    interval(b0, b1, &lo, &hi);
-    if (two) {
-      interval(b_k, b_k, &lo2, &hi2);
-      if (hi2 >= lo || hi2 == 0xffffffffu) {  // they meet: one
-        lo = min(lo, lo2);
-        hi = max(hi, hi2);
-        lo2 = lo;
-        hi2 = hi;
-      }
-    }
-    const float f_lo = from_orderable(lo), f_lo2 = two ? from_orderable(lo2) : INFINITY;
-    const float f_hi = hi == 0xffffffffu ? INFINITY : from_orderable(hi), f_hi2 = hi2 == 0xffffffffu ? INFINITY : from_orderable(hi2);
-    if (tid == 0) sh.n_list = 0;
-    __syncthreads();
-    // ---- the pass in fp64: mass and number above the interval, and above the second one (without top-k: of all)
-    double above = 0.0, above2 = 0.0;
-    int n_above = 0, n_above2 = 0;
-    const float near = near_from();
-    along([&](const uint4& v, int at) {
-      float x[E];
-      double w[E];
-      raw_of(v, near, x, w);
-      bool in = false;
-#pragma unroll
-      for (int e = 0; e < E; ++e) {
-        const bool a1 = x[e] > f_hi;
-        above += a1 ? w[e] : 0.0;
-        n_above += a1;
-        in |= !a1 && x[e] >= f_lo;
-      }
-      if (p) {
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const bool a2 = x[e] > f_hi2;
-          above2 += a2 ? w[e] : 0.0;
-          n_above2 += a2;
-          in |= !a2 && x[e] >= f_lo2;
+    // (a border that the estimate puts next to where it is, is looked for in the bins there)
+#pragma unroll 1
+    for (int turn_ = 0; turn_ < 4; ++turn_) {
+      uint32_t lo, hi, lo2 = 0xffffffffu, hi2 = orderable(-INFINITY);  // (the second one holds nothing)
+      interval(b0, b1, &lo, &hi);
+      if (two) {
+        interval(b_k, b_k, &lo2, &hi2);
+        if (hi2 >= lo || hi2 == 0xffffffffu) {  // they meet: one
+          lo = min(lo, lo2);
+          hi = max(hi, hi2);
+          lo2 = lo;
+          hi2 = hi;
         }
       }
-      if (in) {
-#pragma unroll
-        for (int e = 0; e < E; ++e)
-          if ((x[e] >= f_lo && x[e] <= f_hi) || (x[e] >= f_lo2 && x[e] <= f_hi2)) {
-            const int i = atomicAdd(&sh.n_list, 1);
-            if (i < kList) sh.list[i] = make_key(x[e], at * E + e);
-          }
-      }
-    });
-    out->run = above;
-    const Mail r = reduce(above, above2, n_above, n_above2);
-    const int n_all = join();
-    if (n_all > kList) return;
-    uint64_t* list = tokens();
-    sort(list, n_all);
-    // ---- the list: first the interval's, then (with both limits) the second one's
-    const int each_thread = (n_all + kThreads - 1) / kThreads;
-    double w[kEach], of_mine = 0.0, all;
-    int first_n = 0, later = 0;  // tokens of the interval; tokens above the second one
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = tid * each_thread + e;
-      w[e] = 0.0;
-      if (e < each_thread && i < n_all) {
-        const uint32_t key = static_cast<uint32_t>(list[i] >> 32);
-        w[e] = raw(from_orderable(key));
-        sh.scan[i] = w[e];
-        first_n += key >= lo;
-        later += key > hi2;
-      }
-      of_mine += w[e];
-    }
-    const double before = before_cta(of_mine, &all);
-    first_n = sum_cta(first_n | later << 16);
-    later = first_n >> 16;
-    first_n &= 0xffff;
-    // mass of the first top_k: what lies above the second interval, and the first of its tokens
-    double mass = r.b;
-    const int of2 = top_k - r.m;
-    if (two) {
-      if (of2 < 1 || later + of2 > n_all) return;
-      double acc = before;
-      if (tid == 0) sh.value2 = 0.0;
+      const float f_lo = from_orderable(lo), f_lo2 = two ? from_orderable(lo2) : INFINITY;
+      const float f_hi = hi == 0xffffffffu ? INFINITY : from_orderable(hi), f_hi2 = hi2 == 0xffffffffu ? INFINITY : from_orderable(hi2);
+      if (tid == 0) sh.n_list = 0;
       __syncthreads();
+      // ---- the pass in fp64: mass and number above the interval, and above the second one (without top-k: of all)
+      double above = 0.0, above2 = 0.0;
+      int n_above = 0, n_above2 = 0;
+      const float near = near_from();
+      along([&](const uint4& v, int at) {
+        float x[E];
+        double w[E];
+        raw_of(v, near, x, w);
+        bool in = false;
+        if (p) {  // (what lies above the second interval is more)
+#pragma unroll
+          for (int e = 0; e < E; ++e) {
+            const bool a2 = x[e] > f_hi2;
+            w[e] = a2 ? w[e] : 0.0;
+            n_above2 += a2;
+            in |= !a2 && x[e] >= f_lo2;
+          }
+          above2 += sum_of(w);
+        }
+#pragma unroll
+        for (int e = 0; e < E; ++e) {
+          const bool a1 = x[e] > f_hi;
+          w[e] = a1 ? w[e] : 0.0;
+          n_above += a1;
+          in |= !a1 && x[e] >= f_lo;
+        }
+        above += sum_of(w);
+        if (in) {
+#pragma unroll
+          for (int e = 0; e < E; ++e)
+            if ((x[e] >= f_lo && x[e] <= f_hi) || (x[e] >= f_lo2 && x[e] <= f_hi2)) {
+              const int i = atomicAdd(&sh.n_list, 1);
+              if (i < kList) sh.list[i] = make_key(x[e], at * E + e);
+            }
+        }
+      });
+      out->run = above;
+      const Mail r = reduce(above, above2, n_above, n_above2);
+      const int n_all = join();
+      if (n_all > kList) return;
+      uint64_t* list = tokens();
+      sort(list, n_all);
+      // ---- the list: first the interval's, then (with both limits) the second one's
+      const int each_thread = (n_all + kThreads - 1) / kThreads;
+      double w[kEach], of_mine = 0.0, all;
+      int first_n = 0, later = 0;  // tokens of the interval; tokens above the second one
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        const int i = tid * each_thread + e;
+        w[e] = 0.0;
+        if (e < each_thread && i < n_all) {
+          const uint32_t key = static_cast<uint32_t>(list[i] >> 32);
+          w[e] = raw(from_orderable(key));
+          sh.scan[i] = w[e];
+          first_n += key >= lo;
+          later += key > hi2;
+        }
+        of_mine += w[e];
+      }
+      const double before = before_cta(of_mine, &all);
+      first_n = sum_cta(first_n | later << 16);
+      later = first_n >> 16;
+      first_n &= 0xffff;
+      // mass of the first top_k: what lies above the second interval, and the first of its tokens
+      double mass = r.b;
+      const int of2 = top_k - r.m;
+      if (two) {
+        if (of2 < 1 || later + of2 > n_all) return;
+        double acc = before;
+        if (tid == 0) sh.value2 = 0.0;
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < kEach; ++e) {
+          const int i = tid * each_thread + e;
+          acc += w[e];
+          if (e < each_thread && i < n_all) {
+            if (i == later - 1) sh.value2 = acc;
+            if (i == later + of2 - 1) sh.value = acc;
+          }
+        }
+        __syncthreads();
+        mass = r.b + (sh.value - sh.value2);
+      }
+      const double goal = static_cast<double>(top_p) * mass;
+      int below = 0, heavy = 0;
+      double acc = r.a + before;
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
         const int i = tid * each_thread + e;
         acc += w[e];
-        if (e < each_thread && i < n_all) {
-          if (i == later - 1) sh.value2 = acc;
-          if (i == later + of2 - 1) sh.value = acc;
+        if (e < each_thread && i < first_n) {
+          below += acc < goal;
+          heavy += w[e] >= static_cast<double>(floor);
+        }
+      }
+      below = sum_cta(below | heavy << 16);
+      heavy = below >> 16;
+      below &= 0xffff;
+      int stay = first_n + 1;  // (more than the interval holds)
+      bool higher = false;     // the border lies above the interval
+      if (k) {
+        stay = min(stay, top_k - r.n);
+        higher |= top_k - r.n < 1;
+      }
+      if (p) {
+        stay = min(stay, below + 1);
+        higher |= r.n > 0 && r.a >= goal;
+      }
+      if (floor > 0.f) {
+        if (heavy < first_n || raw(from_orderable(lo)) < static_cast<double>(floor)) stay = min(stay, heavy);
+        higher |= heavy == 0 && (r.n == 0 || raw(f_hi) < static_cast<double>(floor));
+      }
+      if (higher || stay > first_n) {
+        if (higher ? b0 == 0 : b1 >= kWideBins - 2) return;
+        if (higher) {
+          b1 = b0 - 1;
+          b0 = max(b1 - 3, 0);
+        } else {
+          b0 = b1 + 1;
+          b1 = min(b0 + 3, kWideBins - 2);
+        }
+        __syncthreads();
+        continue;
+      }
+      __syncthreads();
+      if (tid == 0) {  // (of the interval none: what lies above it)
+        sh.value = r.a;
+        sh.cut.border = static_cast<uint64_t>(hi) + 1 << 32;
+      }
+      __syncthreads();
+      acc = r.a + before;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        acc += w[e];
+        if (e < each_thread && tid * each_thread + e == stay - 1) {
+          sh.value = acc;
+          sh.cut.border = list[stay - 1];
         }
       }
       __syncthreads();
-      mass = r.b + (sh.value - sh.value2);
+      out->ok = true;
+      out->n = r.n + stay;
+      out->listed = stay;
+      out->border = sh.cut.border;
+      out->total = sh.value;
+      return;
     }
-    const double goal = static_cast<double>(top_p) * mass;
-    int below = 0, heavy = 0;
-    double acc = r.a + before;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = tid * each_thread + e;
-      acc += w[e];
-      if (e < each_thread && i < first_n) {
-        below += acc < goal;
-        heavy += w[e] >= static_cast<double>(floor);
-      }
-    }
-    below = sum_cta(below | heavy << 16);
-    heavy = below >> 16;
-    below &= 0xffff;
-    int stay = first_n + 1;  // (more than the interval holds)
-    bool higher = false;     // the border lies above the interval
-    if (k) {
-      stay = min(stay, top_k - r.n);
-      higher |= top_k - r.n < 1;
-    }
-    if (p) {
-      stay = min(stay, below + 1);
-      higher |= r.n > 0 && r.a >= goal;
-    }
-    if (floor > 0.f) {
-      if (heavy < first_n || raw(from_orderable(lo)) < static_cast<double>(floor)) stay = min(stay, heavy);
-      higher |= heavy == 0 && (r.n == 0 || raw(f_hi) < static_cast<double>(floor));
-    }
-    if (higher || stay > first_n) return;
-    __syncthreads();
-    if (tid == 0) {  // (of the interval none: what lies above it)
-      sh.value = r.a;
-      sh.cut.border = static_cast<uint64_t>(hi) + 1 << 32;
-    }
-    __syncthreads();
-    acc = r.a + before;
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      acc += w[e];
-      if (e < each_thread && tid * each_thread + e == stay - 1) {
-        sh.value = acc;
-        sh.cut.border = list[stay - 1];
-      }
-    }
-    __syncthreads();
-    out->ok = true;
-    out->n = r.n + stay;
-    out->listed = stay;
-    out->border = sh.cut.border;
-    out->total = sh.value;
   }
   // The token of such a row.  taken(lo, hi): mass that is taken out of ids lo .. hi-1.
   template <typename G, typename F>
