@@ -11,10 +11,19 @@
 // hold (a slot is a bucket that tokens fall into by chance: with J of B slots reaching the value, about
 // -B ln(1 - J/B) tokens do), and so a value that all that stays lies above.  The few slots that reach it are
 // read again, their tokens above it make a list, and the list is sorted, summed in fp64 and cut.  Rows of which
-// more stays than the list holds go another way (see wide_border).
+// more stays than the list holds are counted into 2048 bins, summed in fp64 above the bin of the border, and only that bin's
+// tokens are listed (Row::wide); where these are too many as well, the interval is narrowed (Row::wide_border).
 //
 // Decisions are those of fp64 sums.  The whole mass is summed in fp32 with a bound on its error (kSlack); a decision that
 // it could turn is taken again after the row has been summed in fp64.
+//
+// Many rows have a CTA each, which leaves to a second kernel's clusters what the list or the fp32 sums cannot tell.
+//
+// What bounds it, as measured on a B200: a row of 128 256 bf16 of which a list's worth stays takes 12 us with its launch (eight
+// CTAs: 3 us of reading, then a chain of some ten barriers and exchanges of 0.5 us each); one of which thousands stay 35 us,
+// most of it two more passes, one of shared-memory atomics and one of fp64 (64 lanes a cycle and SM, 20 instructions a
+// token).  512 such rows with mixed limits take 118 us (131 MB at 1.1 TB/s): the first kernel 53 us, of which 20 us is the
+// reading at 6.6 TB/s and 8 us the exponentials, the second 65 us for the few per cent of rows that it is left.
 #pragma once
 
 #include <algorithm>
@@ -119,7 +128,7 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
     uint64_t border = 0;
     bool listed = false, exact = false;
     typename R::Wide wide;
-    wide.ok = false;
+    wide.ok = wide.near = false;
     double total = 1.0;
     int n_stay = 1;
     if (greedy) {
@@ -178,40 +187,41 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
         }
       }
       if constexpr (kServesAll) {
-      if (!listed && !wide.ok) {
+        if (!listed && !wide.ok) {
+          const float from = row.near_from();
 #pragma unroll 1
-        for (int kind = 0; kind < 2; ++kind) {
-          if (kind == 0 ? top_k == 0 : !(top_p < 1.f)) continue;
-          double goal = 0.0;
-          if (kind == 1) {
-            double m = 0.0;
-            row.each([&](float x, int id) { m += x > -INFINITY && make_key(x, id) >= border ? row.raw(x) : 0.0; });
-            goal = static_cast<double>(top_p) * row.reduce(m, 0.0, 0, 0).a;
+          for (int kind = 0; kind < 2; ++kind) {
+            if (kind == 0 ? top_k == 0 : !(top_p < 1.f)) continue;
+            double goal = wide.goal;
+            if (kind == 1 && !wide.near) {
+              double m = 0.0;
+              row.each([&](float x, int id) { m += x > -INFINITY && make_key(x, id) >= border ? row.raw_any(x, from) : 0.0; });
+              goal = static_cast<double>(top_p) * row.reduce(m, 0.0, 0, 0).a;
+            }
+            border = row.wide_border(border, kind == 0 ? top_k : 0, goal, wide);
           }
-          border = row.wide_border(border, kind == 0 ? top_k : 0, goal);
-        }
-        const double least = static_cast<double>(floor);
-        double m = 0.0;
-        int n = 0;
-        uint32_t low = 0xffffffffu;  // the lowest value that min-p leaves
-        row.each([&](float x, int id) {
-          if (x == -INFINITY || make_key(x, id) < border) return;
-          const double w = row.raw(x);
-          if (w < least) return;
-          m += w;
-          ++n;
-          low = min(low, orderable(x));
-        });
+          const double least = static_cast<double>(floor);
+          double m = 0.0;
+          int n = 0;
+          uint32_t low = 0xffffffffu;  // the lowest value that min-p leaves
+          row.each([&](float x, int id) {
+            if (x == -INFINITY || make_key(x, id) < border) return;
+            const double w = row.raw_any(x, from);
+            if (w < least) return;
+            m += w;
+            ++n;
+            low = min(low, orderable(x));
+          });
           const auto r = row.reduce(m, 0.0, n, 0);
-        uint32_t unused = 0;
-        row.least_most(&low, &unused);
-        total = r.a;
-        n_stay = r.n;
-        if (floor > 0.f) {
-          const uint64_t f = static_cast<uint64_t>(low) << 32;  // with any id
-          border = f > border ? f : border;
+          uint32_t unused = 0;
+          row.least_most(&low, &unused);
+          total = r.a;
+          n_stay = r.n;
+          if (floor > 0.f) {
+            const uint64_t f = static_cast<uint64_t>(low) << 32;  // with any id
+            border = f > border ? f : border;
+          }
         }
-      }
       }
     }
     const auto weight = [&](float x, int id) { return x > -INFINITY && make_key(x, id) >= border ? row.raw(x) : 0.0; };
@@ -457,16 +467,24 @@ cudaError_t launch(K kernel, const LimitedArgs& a, int64_t rows, int cluster, in
 template <typename T>
 cudaError_t limited_as(const LimitedArgs& a, bool tree, int sms, cudaStream_t stream, int64_t* launches) {
   if (tree) return launch(limited_kernel<T, 8, true>, a, a.N, 8, kClusterThreads, false, stream, launches);
-  // As many CTAs a row as fit the device twice over; one where there are rows enough, and then the few that need more
-  // than it can tell by clusters.
-  if (a.N * 8ll <= 2ll * sms) return launch(limited_kernel<T, 8, false>, a, a.N, 8, kClusterThreads, false, stream, launches);
+  // As many CTAs a row as fit the device twice over; one where there are rows enough, and then the few that need more than it can
+  // tell by clusters.  A cluster's exchanges cost more than its CTAs save where the row is short.  Measured, in us, for rows that
+  // mix limits (in brackets: all top-k 50):
+  //   of 128 256 bf16     8: 55 (16) by eight, 66 (16) by four, 82 (31) by one; 37: 51 (27), 64 (18), 84 (31);
+  //                       74: 59 (39), 66 (29), 100 (31); 148: 102 (61), 84 (41), 107 (31); 300: 170 (117), 119 (68), 113 (35)
+  //   of 32 000 f16       8: 45 (14), 29 (14), 45 (21); 74: 57 (35), 35 (23), 49 (21); 148: 94 (57), 47 (33), 59 (21); 300: by one 74 (23)
+  const bool brief = a.V <= (128 << 10) / static_cast<int>(16 / T::kPerVec);
+  if (!brief && a.N * 8ll <= 2ll * sms) return launch(limited_kernel<T, 8, false>, a, a.N, 8, kClusterThreads, false, stream, launches);
   if (a.N * 4ll <= 2ll * sms) return launch(limited_kernel<T, 4, false>, a, a.N, 4, kClusterThreads, false, stream, launches);
-  // (ten small CTAs an SM where they have work, else five with as many loads on their way)
-  const bool small = a.N > 5ll * sms;
+  // Ten small CTAs an SM where they have work and only the rows' sums to make, else five with as many loads on their way: of
+  // 128 256 bf16 1000 rows without limits take 92 us with 128 threads and 109 with 256, with top-k 50 82 and 74.
+  const bool small = a.N > 5ll * sms && !a.top_k && !a.top_p && !a.min_p;
   const cudaError_t e = small ? launch(many_rows_kernel<T, 128>, a, a.N, 1, 128, false, stream, launches)
                               : launch(many_rows_kernel<T, 256>, a, a.N, 1, 256, false, stream, launches);
   if (e != cudaSuccess) return e;
-  // (73 clusters on a B200: a number by which settings that repeat fall to all)
+  // What is left, by clusters of two where rows are short and of four where they are long: 512 mixed rows of 32 000 f16 take 74
+  // and 88 us, 148 of 128 256 bf16 131 and 107.  (An odd number of clusters: settings that repeat fall to all of them.)
+  if (brief) return launch(left_rows_kernel<T, 2>, a, std::max(sms * 2 / 2 - 1, 1), 2, kClusterThreads, true, stream, launches);
   return launch(left_rows_kernel<T, 4>, a, std::max(sms * 2 / 4 - 1, 1), 4, kClusterThreads, true, stream, launches);
 }
 

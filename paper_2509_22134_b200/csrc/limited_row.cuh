@@ -111,7 +111,6 @@ struct Shared {
   int red_n[2][kWarps];
   int n_list, bin, bin2, from, enough;
   float tau;
-  uint32_t key_lo, key_hi;
   double value, value2;
   Cut cut;
   double pow2[kServesAll ? 32 : 1];  // 2^(j/32)
@@ -194,6 +193,8 @@ struct Row {
   __device__ __forceinline__ float near_from() const {
     return fmaxf(static_cast<float>(static_cast<double>(M) - 999.0 / scale), -3.4028235e38f);
   }
+
+  __device__ __forceinline__ double raw_any(float x, float from) const { return x >= from ? raw_near(x) : 0.0; }
 
   // f(vector, its number) over the thread's vectors; the next three are on their way meanwhile.
   template <typename F>
@@ -820,7 +821,7 @@ struct Row {
   // The entry of kMails (in the order of CTAs and warps) that holds aim: the last one with a mass that begins at or below
   // it, among several rows of entries one after the other.  mass(row, i); returns row * kMails + i, or -1; *begin: where it begins.
   template <int kRows, typename F>
-  __device__ __forceinline__ int holder(double at, double aim, F mass, double* begin, double* end) {
+  __device__ __forceinline__ int holder(double at, double aim, F mass, double* begin) {
     int found = -1;
 #pragma unroll
     for (int q = 0; q < kRows; ++q)
@@ -838,7 +839,6 @@ struct Row {
         }
         at += __shfl_sync(kFull, upto, 31);
       }
-    *end = at;
     return found;
   }
 
@@ -929,9 +929,9 @@ struct Row {
     s.c = __shfl_sync(kFull, upto[2], 31);
     s.d = __shfl_sync(kFull, upto[3], 31);
     const Mail* all = post(s);
-    double begin = 0.0, end;
+    double begin = 0.0;
     const int held = holder<kUnroll>(at, aim, [&](int q, int i) { return q == 0 ? all[i].a : q == 1 ? all[i].b : q == 2 ? all[i].c : all[i].d; },
-                                     &begin, &end);
+                                     &begin);
     if (held < 0) {
       f.mine = rank == 0 && tid == 0;
       return f;
@@ -972,20 +972,21 @@ struct Row {
     return f;
   }
 
-  // ---- runs: a thread's share of the row's ids, one after the other
-  __device__ __forceinline__ void run_of(int* lo, int* hi) const {  // in vectors
+  // ---- ranges: a warp's share of the row's ids, one after the other.  (Its lanes stand side by side: with a run of ids for every
+  // thread the pass in fp64 over a row of 128 256 took 10.9 us in place of 7.4.)
+  __device__ __forceinline__ void range_of(int w, int* lo, int* hi) const {  // in vectors
     const int per = (nvec + kCluster - 1) / kCluster;
     const int vec0 = min(rank * per, nvec), vecs = min(vec0 + per, nvec) - vec0;
-    const int run = (vecs + kThreads - 1) / kThreads;
-    *lo = vec0 + min(tid * run, vecs);
-    *hi = min(*lo + run, vec0 + vecs);
+    const int range = (vecs + kWarps - 1) / kWarps;
+    *lo = vec0 + min(w * range, vecs);
+    *hi = min(*lo + range, vec0 + vecs);
   }
-  // f(vector, its number) over the thread's run.
+  // f(vector, its number) over the thread's part of its warp's range.
   template <typename F>
   __device__ __forceinline__ void along(F f) const {
     int lo, hi;
-    run_of(&lo, &hi);
-    ahead([&](int i) { return lo + i; }, hi - lo, f);
+    range_of(warp, &lo, &hi);
+    ahead([&](int i) { return lo + lane + 32 * i; }, (hi - lo - lane + 31) / 32, f);
   }
   // fp64 weights of the tokens of a vector; from: near_from().
   __device__ __forceinline__ void raw_of(const uint4& v, float from, float (&x)[E], double (&w)[E]) const {
@@ -1011,13 +1012,13 @@ struct Row {
     });
     return reduce(m, 0.0, 0, 0).a;
   }
-  // Of the runs' masses `mine`: the first id at which the cumulative sum of weight(value, id) passes u * (the whole sum),
-  // or `aim` where u < 0.  Found in one lane of the cluster; id -1 where nothing has a weight.
+  // Of the mass of every warp's range (sum over the lanes of `mine`): the first id at which the cumulative sum of
+  // weight(value, id) passes u * (the whole sum), or `aim` where u < 0; the range that holds it is read again.  Found in one
+  // thread of the cluster; id -1 where nothing has a weight.
   template <typename F>
   __device__ __forceinline__ Found pick(double mine, F weight, double u, double aim) {
-    const double upto = scan_warp(mine, lane);
     Mail s{};
-    s.a = __shfl_sync(kFull, upto, 31);
+    s.a = sum_warp(mine);
     const Mail* all = post(s);
     double total = 0.0;
 #pragma unroll
@@ -1025,20 +1026,32 @@ struct Row {
     total = sum_warp(total);
     if (u >= 0.0) aim = u * total;
     Found f{total, 0.0, -1, false, false};
-    double begin = 0.0, end;
-    const int held = holder<1>(0.0, aim, [&](int, int i) { return all[i].a; }, &begin, &end);
+    double begin = 0.0;
+    const int held = holder<1>(0.0, aim, [&](int, int i) { return all[i].a; }, &begin);
     if (held < 0) {
       f.mine = rank == 0 && tid == 0;
       return f;
     }
-    if (held != rank * kWarps + warp) return f;
-    const double start = begin + (upto - mine);
-    const unsigned some = __ballot_sync(kFull, mine > 0.0), is = __ballot_sync(kFull, mine > 0.0 && start <= aim);
-    const int from = is ? 31 - __clz(is) : __ffs(some) - 1;  // (rounding: then the first that holds something)
+    if (held / kWarps != rank) return f;
+    // the CTA's threads have runs of that range
     int lo, hi;
-    run_of(&lo, &hi);
-    const int e_lo = __shfl_sync(kFull, lo, from) * E, e_hi = __shfl_sync(kFull, hi, from) * E;
-    double acc = __shfl_sync(kFull, start, from);
+    range_of(held % kWarps, &lo, &hi);
+    const int run = (hi - lo + kThreads - 1) / kThreads, v0 = min(lo + tid * run, hi), v1 = min(v0 + run, hi);
+    double of_run = 0.0, unused;
+    for (int id = v0 * E; id < v1 * E; ++id) of_run += weight(T::load1(z, id), id);
+    if (tid == 0) sh.from = -1;
+    const double start = begin + before_cta(of_run, &unused);
+    if (of_run > 0.0 && start <= aim) atomicMax(&sh.from, tid);
+    __syncthreads();
+    const bool none = sh.from < 0;  // (rounding: then the first that holds something)
+    __syncthreads();
+    if (none && of_run > 0.0) atomicMax(&sh.from, kThreads + (kThreads - 1 - tid));
+    __syncthreads();
+    const int from = sh.from >= kThreads ? 2 * kThreads - 1 - sh.from : sh.from;
+    if (warp != from / 32) return f;
+    // the tokens of that run, by the warp of its thread
+    const int e_lo = __shfl_sync(kFull, v0, from & 31) * E, e_hi = __shfl_sync(kFull, v1, from & 31) * E;
+    double acc = __shfl_sync(kFull, start, from & 31);
     for (int e0 = e_lo; e0 < e_hi; e0 += 32) {
       const int id = e0 + lane;
       const double w = id < e_hi ? weight(T::load1(z, id), id) : 0.0;
@@ -1086,14 +1099,17 @@ struct Row {
   }
 
   // ---- rows of which more stays than a list holds: the tokens are counted by their distance from the largest logit, which
-  // tells where the border lies to a bin; one pass in fp64 then sums what lies above that interval, run by run, and
+  // tells where the border lies to a bin; one pass in fp64 then sums what lies above that interval, range by range, and
   // lists what lies in it.  All that is decided is decided by these sums; where the border does not lie in the interval, or
   // that holds too many, ok is false.
   struct Wide {
     bool ok;
     int n, listed;      // tokens that stay, how many of them in the list
     uint64_t border;
-    double total, run;  // mass of what stays; of the thread's run above the interval
+    double total, run;  // mass of what stays; of the thread's part of its warp's range above the interval
+    bool near;          // not ok for more tokens than a list holds between these values, and the mass looked for
+    uint32_t lo, hi;
+    double goal;
   };
   // Values from bin b0 to bin b1 (a little more: what rounds is looked at, not trusted).
   __device__ __forceinline__ void interval(int b0, int b1, uint32_t* lo, uint32_t* hi) const {
@@ -1133,7 +1149,7 @@ struct Row {
   }
   __device__ __forceinline__ void wide(int top_k, float top_p, float floor, Wide* out) {
     constexpr int kOf = kWideBins / kThreads;
-    out->ok = false;
+    out->ok = out->near = false;
     const float unit = fminf(static_cast<float>(scale), 1e30f);
     // bins of 1/64 in log2 units, the last one for all from 32 on
     clear_bins();
@@ -1262,7 +1278,13 @@ struct Row {
       out->run = above;
       const Mail r = reduce(above, above2, n_above, n_above2);
       const int n_all = join();
-      if (n_all > kList) return;
+      if (n_all > kList) {
+        out->near = top_k == 0 || !p;
+        out->lo = lo;
+        out->hi = hi;
+        out->goal = static_cast<double>(top_p) * r.b;
+        return;
+      }
       uint64_t* list = tokens();
       sort(list, n_all);
       // ---- the list: first the interval's, then (with both limits) the second one's
@@ -1374,29 +1396,33 @@ struct Row {
   // The token of such a row.  taken(lo, hi): mass that is taken out of ids lo .. hi-1.
   template <typename G, typename F>
   __device__ __forceinline__ Found draw_wide(const Wide& of, double u, G taken, F weight) {
-    by_id(of.listed);
     const uint64_t* list = tokens();
-    int v0, v1;
-    run_of(&v0, &v1);
-    const auto id_of = [&](int i) { return static_cast<int>(0xffffffffu - static_cast<uint32_t>(list[i] >> 32)); };
-    int at = 0;
-    for (int step = kList; step > 0; step /= 2)
-      if (at + step <= of.listed && id_of(at + step - 1) < v0 * E) at += step;
+    int lo, hi;
+    range_of(warp, &lo, &hi);
     double run = of.run;
-    for (; at < of.listed && id_of(at) < v1 * E; ++at) run += sh.scan[static_cast<uint32_t>(list[at])];
-    const double gone = v1 > v0 ? taken(v0 * E, v1 * E) : 0.0;
-    if (gone > 0.0) {  // (exactly: it may be all that the run holds)
-      run = 0.0;
-      for (int id = v0 * E; id < v1 * E; ++id) run += weight(T::load1(z, id), id);
+    for (int i = lane; i < of.listed; i += 32) {
+      const int id = key_id(list[i]);
+      if (id >= lo * E && id < hi * E) run += sh.scan[i];
+    }
+    const double gone = hi > lo ? taken(lo * E, hi * E) : 0.0;
+    if (gone > 0.0) {
+      const double rest = sum_warp(run) - gone;
+      run = lane == 0 ? rest : 0.0;
+      if (rest < 1e-4 * gone) {  // (few digits of it are left, it may be nothing: added up without what is taken out)
+        run = 0.0;
+#pragma unroll 1
+        for (int id = lo * E + lane; id < hi * E; id += 32) run += weight(T::load1(z, id), id);
+      }
     }
     return pick(run, weight, u, 0.0);
   }
 
   // ---- rows of which much stays.  The border of a count of tokens (goal_n > 0) or of a mass, among those at or above `kept`:
   // an interval of values is narrowed to the border's, first by the tokens' distances from the row's largest logit,
-  // then by equal parts of what is left, until a list takes its tokens or they are all equal.
-  __device__ __forceinline__ uint64_t wide_border(uint64_t kept, int goal_n, double goal) {
+  // then (of.near: from there on) by equal parts of what is left, until a list takes its tokens or they are all equal.
+  __device__ __forceinline__ uint64_t wide_border(uint64_t kept, int goal_n, double goal, const Wide& of) {
     const bool by_n = goal_n > 0;
+    const float from = near_from();
     const float unit = fminf(static_cast<float>(scale), 1e30f);
     // The bin at which the count, or about the mass, is reached: (bin, tokens in it).  weight(b): mass of a token in bin b.
     const auto find = [&](auto weight, double n0, double m0, double stretch) {
@@ -1443,19 +1469,22 @@ struct Row {
       flip ^= 1;
       return b;
     };
-    // ---- by distance: bins of 1/64 in log2 units, the last one for all from 32 on
-    clear_bins();
-    each([&](float x, int id) {
-      if (x == -INFINITY || make_key(x, id) < kept) return;
-      const float d = (M - x) * unit;
-      atomicAdd(&sh.wide[d < 31.98f ? static_cast<int>(d * 64.f) : kWideBins - 1], 1);
-    });
-    const int b0 = find([](int b) { return ex2_approx(-(static_cast<float>(b) + 0.5f) * (1.f / 64)); }, 0.0, 0.0, 0.0);
-    // (a little more than the bin: what rounds is looked at, not trusted)
-    const auto value_at = [&](float d) { return M - d / unit; };
-    const float nudge = 1e-6f * (fabsf(M) + 32.f / unit);
-    uint32_t hi = b0 <= 0 ? 0xffffffffu : orderable(value_at(static_cast<float>(b0) * (1.f / 64)) + nudge);
-    uint32_t lo = b0 >= kWideBins - 1 ? 0u : orderable(value_at(static_cast<float>(b0 + 1) * (1.f / 64)) - nudge);
+    uint32_t lo = of.lo, hi = of.hi;
+    if (!of.near) {
+      // ---- by distance: bins of 1/64 in log2 units, the last one for all from 32 on
+      clear_bins();
+      each([&](float x, int id) {
+        if (x == -INFINITY || make_key(x, id) < kept) return;
+        const float d = (M - x) * unit;
+        atomicAdd(&sh.wide[d < 31.98f ? static_cast<int>(d * 64.f) : kWideBins - 1], 1);
+      });
+      const int b0 = find([](int b) { return ex2_approx(-(static_cast<float>(b) + 0.5f) * (1.f / 64)); }, 0.0, 0.0, 0.0);
+      // (a little more than the bin: what rounds is looked at, not trusted)
+      const auto value_at = [&](float d) { return M - d / unit; };
+      const float nudge = 1e-6f * (fabsf(M) + 32.f / unit);
+      hi = b0 <= 0 ? 0xffffffffu : orderable(value_at(static_cast<float>(b0) * (1.f / 64)) + nudge);
+      lo = b0 >= kWideBins - 1 ? 0u : orderable(value_at(static_cast<float>(b0 + 1) * (1.f / 64)) - nudge);
+    }
     for (int turn_ = 0;; ++turn_) {
       // ---- what lies above the interval, and in it
       if (tid == 0) sh.n_list = 0;
@@ -1466,7 +1495,7 @@ struct Row {
       each([&](float x, int id) {
         const uint32_t k = orderable(x);
         if (x == -INFINITY || k < lo || make_key(x, id) < kept) return;
-        const double w = by_n ? 0.0 : raw(x);
+        const double w = by_n ? 0.0 : raw_any(x, from);
         if (k > hi) {
           ++n_above;
           above += w;
@@ -1501,7 +1530,7 @@ struct Row {
         sort(list, n);
         int stay = by_n ? goal_n - s.n : 0;
         if (!by_n) {
-                const int each_thread = (n + kThreads - 1) / kThreads;
+          const int each_thread = (n + kThreads - 1) / kThreads;
           double w[kEach], mine = 0.0, all;
 #pragma unroll
           for (int e = 0; e < kEach; ++e) {

@@ -384,3 +384,74 @@ def test_verify_limited_in_the_layout_of_the_reward_pass(gto):
     # (a node without a row has no children among the nodes)
     for k in out:
         assert torch.equal(out[k], want[k]), k
+
+
+def test_sample_where_nearly_all_rows_need_more_than_a_list(gto):
+    """More rows than are listed for the second kernel: it finds them by their marks; the next call begins anew."""
+    rng = np.random.default_rng(21)
+    V, R, N = 2048, 40, 6000
+    z = dc.round_to(logits(rng, "flat", R, V), "f16")
+    rows, u = rng.integers(0, R, N), rng.random(N).astype(np.float32)
+    s = settings(rng, "p", N, V)
+    s["top_p"] = (0.3 + 0.69 * rng.random(N)).astype(np.float32)
+    ctx, out = run(gto, z, s, u, "f16", rows=rows)
+    assert gto.gto_decode_status(ctx) == 0
+    check(z, s, u, out, rows=rows)
+    for n in (6000, 4097, 4096, 300):
+        _, again = run(gto, z, {k: v[:n] for k, v in s.items()}, u[:n], "f16", ctx=ctx, rows=rows[:n])
+        for k in out:
+            assert np.array_equal(again[k], out[k][:n])
+
+
+def test_two_contexts_draw_on_two_streams_at_once(gto):
+    rng = np.random.default_rng(22)
+    N, V = 200, 16384
+    cfg = gto.make_decode_config(S=N, V_draft=V, V_target=V, logit_dtype="bf16")
+    sets = []
+    for kind in ("power", "flat"):
+        z = dev(dc.round_to(logits(rng, kind, N, V), "bf16"), torch.bfloat16)
+        s, u = {k: dev(v) for k, v in settings(rng, "mixed", N, V).items()}, dev(rng.random(N).astype(np.float32))
+        outs = [[torch.full((N,), -77, dtype=t, device=DEV) for t in (torch.int32, torch.float32, torch.int32)] for _ in range(8)]
+        sets.append((gto.gto_decode_create(cfg, 0), torch.cuda.Stream(DEV), z, s, u, outs))
+    torch.cuda.synchronize()
+    for turn in range(8):
+        for ctx, stream, z, s, u, outs in sets:
+            gto.gto_sample_tokens(ctx, z, s, u, *outs[turn], stream=stream)
+    torch.cuda.synchronize()
+    for ctx, stream, z, s, u, outs in sets:
+        assert gto.gto_decode_status(ctx) == 0
+        for o in outs[1:]:
+            assert all(torch.equal(a, b) for a, b in zip(o, outs[0]))
+        check(z.double().cpu().numpy(), {k: v.cpu().numpy() for k, v in s.items()}, u.cpu().numpy(),
+              dict(zip(("token", "logp", "n_kept"), (t.cpu().numpy() for t in outs[0]))))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("alone", [False, True])
+def test_verify_limited_refuses_a_token_that_is_nearly_all(gto, dtype, alone):
+    """What is left of such a row is a millionth of it, and nothing where the token stood."""
+    rng = np.random.default_rng(23)
+    S, V = 16, 8192
+    c = verify_case(rng, S, 1, 1, V, V, dtype)
+    z = 0.5 * rng.normal(size=(S, 2, V))
+    heavy = rng.integers(0, V, S)
+    for i in range(S):
+        if alone:
+            z[i, 0, max(heavy[i] - 300, 0):heavy[i] + 300] = -np.inf
+        z[i, 0, heavy[i]] = 21.0
+    c["target"] = dc.round_to(z, dtype)
+    c["token"][:, 0], c["parent"][:, 0] = heavy, -1
+    c["u_node"] = np.full((S, 1), 1 - 2.0 ** -24, np.float32)
+    s = dict(temperature=np.ones(S, np.float32), top_k=rng.integers(3000, 7000, S).astype(np.int32))
+    ctx, out, _ = run_tree(gto, c, s, 1, V, V, dtype)
+    assert gto.gto_decode_status(ctx) == 0
+    assert (out["accept_len"] == 0).all() and (out["token"][:, 0] != heavy).all()
+    # (the rest is 1e-6 of the whole, whose sums are good to 1e-15: decisions clearer than 1e-8 of it are told)
+    clear = 0
+    for i in range(S):
+        _, _, last, margin = lim.verify(c["parent"][i], c["token"][i], 1 + np.arange(1), c["target"][i], u_node=c["u_node"][i].astype(float),
+                                        u_bonus=float(c["u_bonus"][i]), D=1, d2t=None, temperature=1.0, top_k=int(s["top_k"][i]))
+        if margin > 1e-8:
+            clear += 1
+            assert out["token"][i, 0] == last
+    assert clear >= 12
