@@ -48,7 +48,8 @@ typedef enum {
   GTO_ERR_BAD_INDEX = 8    /* device status: an index in a caller's table (d2t, a tree's
                               rows, tokens or parents, a path's rows, a page table, the
                               lengths of a batch) was out of range; the
-                              entry was skipped, results that depend on it are unspecified  */,
+                              entry was skipped, results that depend on it are unspecified  */
+  ,
   GTO_ERR_NO_PAGES = 9     /* device status: gto_pages_resize found too few free pages; the
                               sequences that it could not serve are as they were            */
 } gto_status;
@@ -324,7 +325,7 @@ typedef struct gto_decode_ctx gto_decode_ctx;
 enum {
   GTO_DECODE_ROPE_INTERLEAVED = 1u, /* rotate the pairs (2i, 2i+1) instead of (i, i + rope_dims/2) */
   GTO_DECODE_PAGES = 4u, /* the context serves gto_pages_fork, _resize and _compact: 4 (S max_pages + 3 n_pages)
-                            + 32 S bytes more of workspace                                     */
+                            + 32 S bytes more of workspace; S max_pages < 2^31, n_pages <= 2^30 */
   GTO_DECODE_CONTEXT_ROWS = 2u /* gto_verify_tree reads target rows in the layout of
                                   gto_tree_reward, [S, R, V_target] with R = 1 + (D-1)k, through
                                   node_depth and node_slot; default: [S, 1+g, V_target], row 0

@@ -215,8 +215,9 @@ gto_status gto_decode_create(gto_decode_ctx** out, const gto_decode_config* c, i
         c->rope_dims % 16 || c->n_kv_heads > 65535)
       return GTO_ERR_UNSUPPORTED;
     if (static_cast<int64_t>(c->max_pages) * c->page_size > (1ll << 31) - 256) return GTO_ERR_UNSUPPORTED;
-    // the page calls have a copy of the table
-    if ((c->flags & GTO_DECODE_PAGES) && static_cast<int64_t>(c->S) * c->max_pages > (1ll << 33)) return GTO_ERR_UNSUPPORTED;
+    // the page calls count slots and pages in 32 bits
+    if ((c->flags & GTO_DECODE_PAGES) && (static_cast<int64_t>(c->S) * c->max_pages >= (1ll << 31) || c->n_pages > (1 << 30)))
+      return GTO_ERR_UNSUPPORTED;
     // work units of a call are counted in 32 bits
     if (static_cast<int64_t>(c->T) * c->n_q_heads + c->S >= (1ll << 30)) return GTO_ERR_UNSUPPORTED;
   }

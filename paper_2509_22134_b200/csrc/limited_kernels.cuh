@@ -425,8 +425,11 @@ __global__ void __launch_bounds__(kClusterThreads, 2) left_rows_kernel(LimitedAr
   const int rank = static_cast<int>(blockIdx.x % kCluster), clusters = static_cast<int>(gridDim.x / kCluster);
   const int left = a.left[0];
   if (left <= kMaxLeft) {
-    for (int i = blockIdx.x / kCluster; i < left; i += clusters)
-      serve<T, kCluster, kClusterThreads, false, kLeft>(a, sh, a.left[kLeftRows + i], rank);
+    for (int i = blockIdx.x / kCluster; i < left; i += clusters) {
+      const int s = a.left[kLeftRows + i];
+      // (always, unless calls that share the workspace ran at once)
+      if (s >= 0 && s < a.N) serve<T, kCluster, kClusterThreads, false, kLeft>(a, sh, s, rank);
+    }
   }
   // the last one to have read the count sets it to 0 for the next call
   if (threadIdx.x == 0) {

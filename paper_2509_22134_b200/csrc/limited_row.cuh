@@ -1279,6 +1279,7 @@ struct Row {
       const Mail r = reduce(above, above2, n_above, n_above2);
       const int n_all = join();
       if (n_all > kList) {
+        cluster_sync();  // (the others may still read this CTA's count, which is begun anew)
         out->near = top_k == 0 || !p;
         out->lo = lo;
         out->hi = hi;
@@ -1359,6 +1360,7 @@ struct Row {
       }
       if (higher || stay > first_n) {
         if (higher ? b0 == 0 : b1 >= kWideBins - 2) return;
+        cluster_sync();  // (as above, and the list)
         if (higher) {
           b1 = b0 - 1;
           b0 = max(b1 - 3, 0);
@@ -1366,7 +1368,6 @@ struct Row {
           b0 = b1 + 1;
           b1 = min(b0 + 3, kWideBins - 2);
         }
-        __syncthreads();
         continue;
       }
       __syncthreads();

@@ -10,6 +10,8 @@ ROWS = dict(S=4, g=3, D=2, V_draft=512, V_target=512, logit_dtype="bf16")
     (dict(ROWS, flags=4), 1),                                           # pages without a cache
     (dict(CACHE, flags=8), 1),
     (dict(CACHE, flags=4, S=1 << 20, max_pages=1 << 14), 2),            # a copy of the table would have 64 GB
+    (dict(CACHE, flags=4, S=1 << 16, max_pages=1 << 15), 2),            # slots are counted in 32 bits
+    (dict(CACHE, flags=4, n_pages=(1 << 30) + 1), 2),
 ])
 def test_configurations_are_refused_without_a_device(kw, code):
     from paper_2509_22134_b200 import binding as gto
