@@ -22,8 +22,8 @@
 // What bounds it, as measured on a B200: a row of 128 256 bf16 of which a list's worth stays takes 12 us with its launch (eight
 // CTAs: 3 us of reading, then a chain of some ten barriers and exchanges of 0.5 us each); one of which thousands stay 35 us,
 // most of it two more passes, one of shared-memory atomics and one of fp64 (64 lanes a cycle and SM, 20 instructions a
-// token).  512 such rows with mixed limits take 118 us (131 MB at 1.1 TB/s): the first kernel 53 us, of which 20 us is the
-// reading at 6.6 TB/s and 8 us the exponentials, the second 65 us for the few per cent of rows that it is left.
+// token).  512 such rows with mixed limits take 102 to 108 us (131 MB at 1.2 TB/s): the first kernel about 45 us, of which 20 us
+// is the reading at 6.6 TB/s and 8 us the exponentials, the second 55 to 60 us for the few per cent of rows that it is left.
 #pragma once
 
 #include <algorithm>
@@ -400,12 +400,17 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
   }
 }
 
+// Row of CTA i of N.  An SM has the CTAs i, i + 148, i + 296, ..., and settings often repeat every 2, 4 or 8 rows: rows in
+// their own order gave some SMs nothing but rows whose weights are summed (exponential units busy 61 % of the time on one SM, 2 % on another;
+// 512 mixed rows of 128 256 bf16: 117 us, so 108).
+__device__ __forceinline__ int spread(int i, int N) { return (i & ~15) + 16 <= N ? (i & ~15) | ((i + (i >> 4)) & 15) : i; }
+
 // One CTA a row, for many rows: what a list of the likeliest tokens, or the sums of the warps, can tell.
 template <typename T, int kThreads>
 __global__ void __launch_bounds__(kThreads, 1280 / kThreads) many_rows_kernel(LimitedArgs a) {
   __shared__ Shared<1, kThreads, false> sh;
   asm volatile("griddepcontrol.launch_dependents;" ::: "memory");  // (the next kernel may get ready)
-  serve<T, 1, kThreads, false, kEasy>(a, sh, static_cast<int>(blockIdx.x), 0);
+  serve<T, 1, kThreads, false, kEasy>(a, sh, spread(static_cast<int>(blockIdx.x), a.N), 0);
 }
 
 constexpr int kClusterThreads = 256;
