@@ -299,6 +299,13 @@ gto_status gto_kernel_times(gto_ctx* ctx, void* stream, double* total_ms, int64_
  *   gto_verify_tree     which drafted tokens the target accepts, and the token after them
  *   gto_kv_commit       moves the accepted tokens' cache entries together
  *
+ * and around it
+ *
+ *   gto_sample_tokens   a token for sequences without a tree, under top-k, top-p and min-p;
+ *                       gto_verify_tree_limited verifies trees under the same limits
+ *   gto_pages_fork, gto_pages_resize, gto_pages_compact
+ *                       who holds which pages of the cache
+ *
  * A batch has S sequences.  Sequence s brings a chunk of n = q_start[s+1] - q_start[s] tokens;
  * kv_len[s] = L counts its cache entries, the chunk's among them, so the chunk owns entries
  * base .. L-1 with base = L - n.  Without a tree the chunk's tokens follow one another (one
@@ -309,7 +316,7 @@ gto_status gto_kernel_times(gto_ctx* ctx, void* stream, double* total_ms, int64_
  * Entry t of sequence s lies in place t % page_size of page page_table[s][t / page_size].
  *
  * The functions take a gto_decode_ctx, which owns the workspace (for bf16 / fp16 caches with heads of 64 or 128 about
- * 20 / 39 MB, whatever the other sizes are) and a status word.  Calls
+ * 20 / 39 MB, whatever the other sizes are; 17 KB where it verifies or draws; see GTO_DECODE_PAGES) and a status word.  Calls
  * through one context share them: order them (one stream, events), and give every stream or
  * captured graph that may run at the same time a context of its own.  The calls can be
  * captured into a CUDA graph, which the context has to outlive; lengths, tables and trees are
