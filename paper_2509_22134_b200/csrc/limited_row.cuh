@@ -1155,7 +1155,7 @@ struct Row {
     clear_bins();
     each([&](float x, int) {
       // (the number of tokens in the upper 12 bits, the sum of their places in the bin, in 256ths, in the lower 20: more
-      // than 4095 tokens in a bin spoil both, which is found out)
+      // than 4095 tokens in a bin spoil both: they then tell of fewer, and what follows from them is looked at)
       const int d = static_cast<int>(fminf((M - x) * (unit * (64.f * 256.f)), kWideBins * 256.f - 1.f));
       if (x > -INFINITY) atomicAdd(&sh.wide[d >> 8], (1u << 20) + (d & 255));
     });
@@ -1328,6 +1328,8 @@ struct Row {
         }
         __syncthreads();
         mass = r.b + (sh.value - sh.value2);
+      } else if (p && top_k > 0 && r.m >= top_k) {
+        return;  // (the bins, spoiled, told of fewer tokens than there are)
       }
       const double goal = static_cast<double>(top_p) * mass;
       int below = 0, heavy = 0;
@@ -1370,6 +1372,7 @@ struct Row {
         }
         continue;
       }
+      if (top_k > 0 && r.n + stay > top_k) return;  // (as above)
       __syncthreads();
       if (tid == 0) {  // (of the interval none: what lies above it)
         sh.value = r.a;
@@ -1426,7 +1429,7 @@ struct Row {
     const float from = near_from();
     const float unit = fminf(static_cast<float>(scale), 1e30f);
     // The bin at which the count, or about the mass, is reached: (bin, tokens in it).  weight(b): mass of a token in bin b.
-    const auto find = [&](auto weight, double n0, double m0, double stretch) {
+    const auto find = [&](auto weight, bool by_n, double goal_n, double n0, double m0, double stretch) {
       join_bins<false>();
       constexpr int kOf = kWideBins / kThreads;
       int n[kOf];
@@ -1479,13 +1482,16 @@ struct Row {
         const float d = (M - x) * unit;
         atomicAdd(&sh.wide[d < 31.98f ? static_cast<int>(d * 64.f) : kWideBins - 1], 1);
       });
-      const int b0 = find([](int b) { return ex2_approx(-(static_cast<float>(b) + 0.5f) * (1.f / 64)); }, 0.0, 0.0, 0.0);
+      const int b0 = find([](int b) { return ex2_approx(-(static_cast<float>(b) + 0.5f) * (1.f / 64)); }, by_n, goal_n, 0.0, 0.0, 0.0);
       // (a little more than the bin: what rounds is looked at, not trusted)
       const auto value_at = [&](float d) { return M - d / unit; };
       const float nudge = 1e-6f * (fabsf(M) + 32.f / unit);
       hi = b0 <= 0 ? 0xffffffffu : orderable(value_at(static_cast<float>(b0) * (1.f / 64)) + nudge);
       lo = b0 >= kWideBins - 1 ? 0u : orderable(value_at(static_cast<float>(b0 + 1) * (1.f / 64)) - nudge);
     }
+    // (bounds that are known, and how often an estimate has missed: then the part with the middle token is taken, every other time)
+    uint32_t lo_known = 0, hi_known = 0xffffffffu;
+    int missed = 0;
     for (int turn_ = 0;; ++turn_) {
       // ---- what lies above the interval, and in it
       if (tid == 0) sh.n_list = 0;
@@ -1514,14 +1520,16 @@ struct Row {
       const bool is_above = s.n > 0 && (by_n ? s.n >= goal_n : s.a >= goal);
       const bool is_in = s.m > 0 && (by_n ? s.n + s.m >= goal_n : s.a + s.b >= goal);
       const bool last_turn = turn_ >= 100;  // (sums of 1e5 terms that round differently: then either is right)
-      if (!last_turn && is_above && hi != 0xffffffffu) {
-        lo = hi + 1;
-        hi = 0xffffffffu;
-        continue;
-      }
-      if (!last_turn && !is_in && lo > 0) {
-        hi = lo - 1;
-        lo = 0;
+      if (!last_turn && ((is_above && hi != 0xffffffffu) || (!is_above && !is_in && lo > 0))) {
+        if (is_above) lo_known = hi + 1;
+        else hi_known = lo - 1;
+        if (lo_known > hi_known) {  // (sums that round differently)
+          lo_known = 0;
+          hi_known = 0xffffffffu;
+        }
+        lo = lo_known;
+        hi = hi_known;
+        ++missed;
         continue;
       }
       if (s.m == 0) return kept;  // (nothing below: all stays)
@@ -1584,7 +1592,7 @@ struct Row {
             const uint64_t far = (static_cast<uint64_t>(i) << shift) + ((1u << shift) >> 1);
             return raw(from_orderable(hi - static_cast<uint32_t>(min(static_cast<uint64_t>(hi - lo), far))));
           },
-          s.n, s.a, s.b);
+          by_n || missed % 2 == 1, by_n ? goal_n : s.n + 0.5 * s.m, s.n, s.a, s.b);
       const uint32_t from = static_cast<uint32_t>(max(b, 0)) << shift;
       const uint32_t top = hi - from;
       lo = top - lo >= (1u << shift) ? top - ((1u << shift) - 1) : lo;

@@ -455,3 +455,35 @@ def test_verify_limited_refuses_a_token_that_is_nearly_all(gto, dtype, alone):
             clear += 1
             assert out["token"][i, 0] == last
     assert clear >= 12
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("N", [2, 60, 160])
+def test_sample_rows_whose_logits_lie_next_to_one_another(gto, dtype, N):
+    """More tokens at one distance from the largest logit than a counter holds; top-k among them, with and without the others."""
+    rng = np.random.default_rng(24)
+    V = 16384
+    z = dc.round_to(0.5 + 0.005 * rng.integers(-1, 2, (N, V)) + 1e-4 * rng.integers(-30, 30, (N, V)), dtype)
+    u = rng.random(N).astype(np.float32)
+    k = rng.integers(5000, 16000, N).astype(np.int32)
+    for more in (dict(), dict(min_p=1e-6), dict(top_p=0.8), dict(top_p=0.999, min_p=0.5)):
+        s = dict(temperature=np.full(N, 0.9, np.float32), top_k=k, **{n: np.full(N, x, np.float32) for n, x in more.items()})
+        ctx, out = run(gto, z, s, u, dtype)
+        assert gto.gto_decode_status(ctx) == 0
+        check(z, s, u, out, least=0.75)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("N", [3, 80])
+def test_sample_cold_rows_with_long_tails(gto, dtype, N):
+    """All the mass in a few tokens, the values far apart: no estimate by distance tells where the mass is."""
+    rng = np.random.default_rng(25)
+    V = 24000
+    z = dc.round_to(np.clip(5 * rng.standard_t(1.5, (N, V)), -6e4, 6e4), dtype)
+    u = rng.random(N).astype(np.float32)
+    for heat in (1e-5, 1e-3, 0.1):
+        s = dict(temperature=np.full(N, heat, np.float32), top_k=rng.integers(2000, 20000, N).astype(np.int32),
+                 top_p=(1 - 1e-3 * rng.random(N)).astype(np.float32))
+        ctx, out = run(gto, z, s, u, dtype)
+        assert gto.gto_decode_status(ctx) == 0
+        check(z, s, u, out)
