@@ -57,6 +57,7 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
   __shared__ int s_child, s_removed_n, s_close;
   const int tid = threadIdx.x, lane = tid & 31;
   R row(sh, a.V, rank);
+  row.alone = kMode == kAll;  // (kLeft: its kernel has waited)
   const bool first = row.rank == 0 && tid == 0;
   if constexpr (kServesAll) row.fill_table();  // (read behind a barrier)
 
@@ -382,7 +383,10 @@ __device__ __forceinline__ void serve(const LimitedArgs& a, Shared<kCluster, kTh
       }
     }
   }
-  if (kCluster > 1) row.cluster_sync();  // nobody leaves while its shared memory is read
+  if (kCluster > 1) {
+    row.meet();          // (where no row was read)
+    row.cluster_sync();  // nobody leaves while its shared memory is read
+  }
   if (row.rank != 0) return;
   if (kTree) {
     if (tid == 0) {
@@ -419,6 +423,7 @@ constexpr int kClusterThreads = 256;
 template <typename T, int kCluster, bool kTree>
 __global__ void __launch_bounds__(kClusterThreads, 2) limited_kernel(LimitedArgs a) {
   __shared__ Shared<kCluster, kClusterThreads, true> sh;
+  Row<T, kCluster, kClusterThreads, true>::begun();
   serve<T, kCluster, kClusterThreads, kTree, kAll>(a, sh, static_cast<int>(blockIdx.x / kCluster), static_cast<int>(blockIdx.x % kCluster));
 }
 
@@ -426,9 +431,12 @@ __global__ void __launch_bounds__(kClusterThreads, 2) limited_kernel(LimitedArgs
 template <typename T, int kCluster>
 __global__ void __launch_bounds__(kClusterThreads, 2) left_rows_kernel(LimitedArgs a) {
   __shared__ Shared<kCluster, kClusterThreads, true> sh;
+  using R = Row<T, kCluster, kClusterThreads, true>;
+  R::begun();
   asm volatile("griddepcontrol.wait;" ::: "memory");
   const int rank = static_cast<int>(blockIdx.x % kCluster), clusters = static_cast<int>(gridDim.x / kCluster);
   const int left = a.left[0];
+  R::wait_for_others();
   if (left <= kMaxLeft) {
     for (int i = blockIdx.x / kCluster; i < left; i += clusters) {
       const int s = a.left[kLeftRows + i];

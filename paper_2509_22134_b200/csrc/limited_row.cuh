@@ -134,6 +134,7 @@ struct Row {
   int nvec, blocks, steps, per_slot, slots;
   int rank, tid, lane, warp;
   int turn, flip;  // of the double-buffered exchanges between CTAs / warps
+  bool alone;      // the other CTAs of the cluster may not have begun yet
   float M;         // the row's largest logit
   double scale;    // to log2 units
   float c2;        // the same in fp32
@@ -151,6 +152,7 @@ struct Row {
     per_slot = (steps + kSlots - 1) / kSlots;
     slots = (steps + per_slot - 1) / per_slot;
     turn = flip = 0;
+    alone = false;
   }
   __device__ __forceinline__ void scale_to(double s) {
     scale = s;
@@ -159,6 +161,20 @@ struct Row {
   __device__ __forceinline__ void cluster_sync() const {
     if (kCluster == 1) __syncthreads();
     else asm volatile("barrier.cluster.arrive.release.aligned;\nbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  // Another CTA's shared memory may be written once that CTA has begun.  Every thread says at its kernel's start that it has,
+  // and waits for the others before its first exchange.
+  static __device__ __forceinline__ void begun() {
+    if (kCluster > 1) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  }
+  static __device__ __forceinline__ void wait_for_others() {
+    if (kCluster > 1) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  }
+  __device__ __forceinline__ void meet() {
+    if (kCluster > 1 && alone) {
+      wait_for_others();
+      alone = false;
+    }
   }
   // Vector that thread t of this CTA has in block q of its blocks; nvec or more: none.
   __device__ __forceinline__ int vec_of(int q, int t) const {
@@ -380,6 +396,7 @@ struct Row {
     s.g = warp_max_f32(most);
     s.n = __any_sync(kFull, bad);
     s.m = __any_sync(kFull, low);
+    meet();  // (the first exchange of every kernel; behind the loads)
     const Mail* all = post(s);
     float top = -INFINITY;
     bad = low = false;
