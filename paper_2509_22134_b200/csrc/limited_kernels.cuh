@@ -437,6 +437,7 @@ __global__ void __launch_bounds__(kClusterThreads, 2) left_rows_kernel(LimitedAr
   const int rank = static_cast<int>(blockIdx.x % kCluster), clusters = static_cast<int>(gridDim.x / kCluster);
   const int left = a.left[0];
   R::wait_for_others();
+  __syncthreads();  // (all of the CTA have read the count before thread 0 says so below)
   if (left <= kMaxLeft) {
     for (int i = blockIdx.x / kCluster; i < left; i += clusters) {
       const int s = a.left[kLeftRows + i];

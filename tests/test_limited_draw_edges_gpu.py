@@ -73,3 +73,20 @@ def test_left_rows_of_which_some_are_not_read(gto, dtype):
             assert gto.gto_decode_status(ctx) == 5
             assert (out["token"][10::7] == -1).all()
             check(z, part, u[:n], out, rows=rows[:n])
+
+
+def test_more_left_rows_than_are_listed_call_after_call(gto):
+    """All CTAs of the second kernel read how many rows are left; the last one sets the number back for the next call."""
+    rng = np.random.default_rng(32)
+    V, R, N = 1024, 16, 4500
+    z = torch.from_numpy(dc.round_to(logits(rng, "flat", R, V), "f16")).to(DEV, torch.float16)
+    rows, u = rng.integers(0, R, N), rng.random(N).astype(np.float32)
+    s = dict(temperature=np.full(N, 1.0, np.float32), top_p=(0.6 + 0.39 * rng.random(N)).astype(np.float32))
+    ctx, first = run(gto, z, s, u, "f16", rows=rows, S=N)
+    assert gto.gto_decode_status(ctx) == 0
+    check(z.double().cpu().numpy(), s, u, first, rows=rows)
+    for turn in range(60):
+        n = N if turn % 3 else 100
+        _, again = run(gto, z, {k: v[:n] for k, v in s.items()}, u[:n], "f16", ctx=ctx, rows=rows[:n])
+        assert all(np.array_equal(again[k], first[k][:n]) for k in first), turn
+    assert gto.gto_decode_status(ctx) == 0
