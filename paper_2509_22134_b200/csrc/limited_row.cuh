@@ -205,9 +205,10 @@ struct Row {
     y *= sh.pow2[k & 31];
     return __hiloint2double(__double2hiint(y) + ((k >> 5) << 20), __double2loint(y));
   }
-  // The value from which on it serves.
+  // The value from which on it serves.  (Rounded up: of cold rows of fp32 a step of the logits is hundreds of halvings, and a value
+  // half a step lower would take exponents below the least one.)
   __device__ __forceinline__ float near_from() const {
-    return fmaxf(static_cast<float>(static_cast<double>(M) - 999.0 / scale), -3.4028235e38f);
+    return fmaxf(__double2float_ru(static_cast<double>(M) - 999.0 / scale), -3.4028235e38f);
   }
 
   __device__ __forceinline__ double raw_any(float x, float from) const { return x >= from ? raw_near(x) : 0.0; }

@@ -90,3 +90,64 @@ def test_more_left_rows_than_are_listed_call_after_call(gto):
         _, again = run(gto, z, {k: v[:n] for k, v in s.items()}, u[:n], "f16", ctx=ctx, rows=rows[:n])
         assert all(np.array_equal(again[k], first[k][:n]) for k in first), turn
     assert gto.gto_decode_status(ctx) == 0
+
+
+def cold_rows(rng, N, V):
+    """fp32 rows whose likely logits lie 0 to 24 steps of fp32 below the largest, the others far below; the temperatures put
+    999 halvings of a weight next to the middle between two such steps, on either side."""
+    z = np.empty((N, V))
+    heat = np.empty(N, np.float32)
+    for i in range(N):
+        top = np.float32(rng.choice([20.0, 60000.0, -3.0, 1.0, 3e-3, -7e5, 1e6]))
+        step = abs(float(top) - float(np.nextafter(top, np.float32(-np.inf))))
+        below = rng.choice([1, 2, 3, 4, 6, 8, 12, 16, 20])
+        heat[i] = (below - 0.5 + rng.choice([-0.02, 0.02, 0.2])) * step / (999 * np.log(2.0))
+        z[i] = float(top) - 1000 * step * (1 + rng.random(V))
+        likely = rng.permutation(V)
+        z[i, likely[:2]] = top
+        for j in range(1, 25):
+            z[i, likely[2 * j:2 * j + 2]] = float(top) - j * step
+    z = z.astype(np.float32).astype(np.float64)
+    return z, heat
+
+
+@pytest.mark.parametrize("N", [3, 60, 170])
+@pytest.mark.parametrize("limits", ["none", "k", "k and p", "k and min", "p", "all"])
+def test_weights_that_vanish_within_a_few_steps_of_fp32(gto, limits, N):
+    rng = np.random.default_rng(33)
+    V = 8192
+    z, heat = cold_rows(rng, N, V)
+    s = dict(temperature=heat)
+    if "k" in limits or limits == "all":
+        s["top_k"] = rng.integers(1500, 7000, N).astype(np.int32)
+    if "p" in limits or limits == "all":
+        s["top_p"] = (1 - 0.3 * rng.random(N)).astype(np.float32)
+    if "min" in limits or limits == "all":
+        s["min_p"] = np.full(N, 1e-3, np.float32)
+    for u in (rng.random(N).astype(np.float32), np.full(N, 0.5 + 2.0 ** -23, np.float32), np.full(N, 0.5 - 2.0 ** -23, np.float32)):
+        ctx, out = run(gto, z, s, u, "f32")
+        assert gto.gto_decode_status(ctx) == 0
+        check(z, s, u, out)
+
+
+@pytest.mark.parametrize("limits", ["none", "k", "k and p"])
+def test_trees_whose_weights_vanish_within_a_few_steps_of_fp32(gto, limits):
+    rng = np.random.default_rng(34)
+    S, g, D, V = 20, 12, 3, 8192
+    c = verify_case(rng, S, g, D, V, V, "f32")
+    for i in range(S):
+        rows, heat = cold_rows(rng, 1, V)
+        c["target"][i] = [rng.permutation(rows[0]) for _ in range(1 + g)]
+        c["temperature"][i] = heat[0]
+        for n in range(g):                     # each node one of its context's two largest
+            context = c["target"][i, 1 + c["parent"][i, n]]
+            c["token"][i, n] = np.flatnonzero(context == context.max())[n % 2]
+    c["u_node"] = (0.5 + rng.choice([-1, 1], (S, g)) * 2.0 ** -rng.integers(2, 22, (S, g))).astype(np.float32)
+    s = dict(temperature=c["temperature"].astype(np.float32))
+    if "k" in limits:
+        s["top_k"] = rng.integers(1500, 7000, S).astype(np.int32)
+    if "p" in limits:
+        s["top_p"] = np.full(S, 0.999, np.float32)
+    ctx, out, _ = run_tree(gto, c, s, D, V, V, "f32")
+    assert gto.gto_decode_status(ctx) == 0
+    check_tree(c, s, out, D)
