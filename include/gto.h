@@ -534,7 +534,8 @@ gto_status gto_pages_resize(gto_decode_ctx* ctx, const gto_page_pool* pool, cons
 /* Moves the pages in use to the front of the cache, in all layers: with *n_used of them, the i-th used page of those from
  * n_used on goes to the i-th free place below n_used.  table_out [S, max_pages] and ref_out [n_pages] receive the pool's table
  * and counts afterwards; the pool itself stays as it is, and valid, until a free page is written: copy them over the
- * pool's arrays to go on with the new places.  The outputs overlap neither one another nor the pool's arrays. */
+ * pool's arrays to go on with the new places.  In a pool without sequences (S = 0) the counts alone are read and written.  The
+ * outputs overlap neither one another nor the pool's arrays. */
 gto_status gto_pages_compact(gto_decode_ctx* ctx, const gto_page_pool* pool, const gto_kv_cache* cache,
                              int32_t* table_out, int32_t* ref_out, int32_t* n_used, void* stream);
 

@@ -55,7 +55,7 @@ struct Array {
 };
 bool over_any(Array out, std::initializer_list<Array> in) {
   for (const Array& x : in)
-    if (x.p && x.bytes && overlap(out.p, out.bytes, x.p, x.bytes)) return true;
+    if (out.bytes && x.p && x.bytes && overlap(out.p, out.bytes, x.p, x.bytes)) return true;
   return false;
 }
 
@@ -160,12 +160,14 @@ gto_status limit_args(const gto_limits* in, gto::LimitedArgs* a) {
   return GTO_OK;
 }
 
-gto_status pool_args(const gto_decode_ctx* ctx, const gto_page_pool* in, gto::PoolArgs* out) {
+// counts: whether the call has to do with the pages themselves, also of a pool without sequences (whose other arrays have no
+// elements and may have no address).
+gto_status pool_args(const gto_decode_ctx* ctx, const gto_page_pool* in, bool counts, gto::PoolArgs* out) {
   const gto_decode_config& c = ctx->cfg;
   if (!in || in->S < 0 || in->S > c.S || !ctx->pages_ws) return GTO_ERR_INVALID_ARG;
   out->S = in->S;
-  if (in->S == 0) return GTO_OK;
-  if (!table(in->page_table, 4) || !table(in->kv_len, 4) || !table(in->held, 4) || !table(in->ref_count, 4))
+  if (in->S == 0 && !counts) return GTO_OK;
+  if ((in->S > 0 && (!table(in->page_table, 4) || !table(in->kv_len, 4) || !table(in->held, 4))) || !table(in->ref_count, 4))
     return GTO_ERR_INVALID_ARG;
   const size_t word = sizeof(int32_t), S = in->S;
   const Array all[4] = {{in->page_table, word * S * c.max_pages}, {in->kv_len, word * S}, {in->held, word * S},
@@ -525,7 +527,7 @@ gto_status gto_pages_fork(gto_decode_ctx* ctx, const gto_page_pool* pool, const 
   if (!ctx) return GTO_ERR_INVALID_ARG;
   CallRange range("gto_pages_fork");
   gto::PoolArgs p{};
-  const gto_status st = pool_args(ctx, pool, &p);
+  const gto_status st = pool_args(ctx, pool, false, &p);
   if (st != GTO_OK) return st;
   if (p.S == 0) return GTO_OK;
   if (!table(parent, 4) || over_pool(ctx, pool, {parent, sizeof(int32_t) * p.S})) return GTO_ERR_INVALID_ARG;
@@ -542,7 +544,7 @@ gto_status gto_pages_resize(gto_decode_ctx* ctx, const gto_page_pool* pool, cons
   CallRange range("gto_pages_resize");
   gto::PoolArgs p{};
   gto::CacheArgs c{};
-  gto_status st = pool_args(ctx, pool, &p);
+  gto_status st = pool_args(ctx, pool, false, &p);
   if (st == GTO_OK) st = cache_args(ctx, cache, &c);
   if (st != GTO_OK) return st;
   if (p.S == 0) return GTO_OK;
@@ -561,11 +563,10 @@ gto_status gto_pages_compact(gto_decode_ctx* ctx, const gto_page_pool* pool, con
   CallRange range("gto_pages_compact");
   gto::PoolArgs p{};
   gto::CacheArgs c{};
-  gto_status st = pool_args(ctx, pool, &p);
+  gto_status st = pool_args(ctx, pool, true, &p);
   if (st == GTO_OK) st = cache_args(ctx, cache, &c);
   if (st != GTO_OK) return st;
-  if (p.S == 0) return GTO_OK;
-  if (!table(table_out, 4) || !table(ref_out, 4) || !table(n_used, 4)) return GTO_ERR_INVALID_ARG;
+  if ((p.S > 0 && !table(table_out, 4)) || !table(ref_out, 4) || !table(n_used, 4)) return GTO_ERR_INVALID_ARG;
   const size_t word = sizeof(int32_t);
   const Array outs[3] = {{table_out, word * p.S * p.max_pages}, {ref_out, word * p.n_pages}, {n_used, word}};
   for (int i = 0; i < 3; ++i)
