@@ -515,7 +515,9 @@ typedef struct {
  * that the parent holds beyond them are not).  What s held is given back.  parent[s] = s: s stays as it is; -1: it
  * becomes empty.  All sequences are read as they were before the call, so any mapping will do (beams that change places).
  * No cache entry is copied: gto_pages_resize does that for a page that is about to be written.  A sequence whose parent
- * is none, or whose or whose parent's numbers contradict one another, is reported (GTO_ERR_BAD_INDEX) and stays as it is.
+ * is none, whose held is out of range, or whose parent's held, kv_len and the pages of its entries contradict one another,
+ * is reported (GTO_ERR_BAD_INDEX) and stays as it is.  What is given back need not be sound: the sequence's own kv_len is not
+ * looked at, and a slot of its own that names no page is reported, and the fork made.  Counts are taken as they are.
  * parent: [S], overlaps none of the pool's arrays. */
 gto_status gto_pages_fork(gto_decode_ctx* ctx, const gto_page_pool* pool, const int32_t* parent, void* stream);
 
@@ -525,8 +527,10 @@ gto_status gto_pages_fork(gto_decode_ctx* ctx, const gto_page_pool* pool, const 
  * holds too get a page of their own, and the first of them the entries below kv_len[s], in all layers (every sequence of the
  * call that shares the page gets a copy; the old page is free if nobody kept it).  New pages are the lowest that were free
  * before the call, in the order of the sequences; what the call gives back can be had by the next one.  A sequence for which
- * too few are left stays as it is, and so do those behind it that need pages (GTO_ERR_NO_PAGES).  A sequence whose numbers contradict one
- * another or whose want is above max_pages * page_size is reported (GTO_ERR_BAD_INDEX) and stays as it is.
+ * too few are left stays as it is, and so do those behind it that need pages (GTO_ERR_NO_PAGES).  A sequence whose held
+ * and kv_len contradict one another, whose want is above max_pages * page_size, or that has a slot to be written that names no page
+ * is reported (GTO_ERR_BAD_INDEX) and stays as it is.  A slot that is given back and names no page is reported, and the call
+ * carried out; slots that stay and are not written are not looked at.  Counts are taken as they are.
  * want: [S], overlaps none of the pool's arrays. */
 gto_status gto_pages_resize(gto_decode_ctx* ctx, const gto_page_pool* pool, const int32_t* want,
                             const gto_kv_cache* cache, void* stream);
@@ -534,7 +538,8 @@ gto_status gto_pages_resize(gto_decode_ctx* ctx, const gto_page_pool* pool, cons
 /* Moves the pages in use to the front of the cache, in all layers: with *n_used of them, the i-th used page of those from
  * n_used on goes to the i-th free place below n_used.  table_out [S, max_pages] and ref_out [n_pages] receive the pool's table
  * and counts afterwards; the pool itself stays as it is, and valid, until a free page is written: copy them over the
- * pool's arrays to go on with the new places.  In a pool without sequences (S = 0) the counts alone are read and written.  The
+ * pool's arrays to go on with the new places.  In a pool without sequences (S = 0) the counts alone are read and written.  A
+ * held slot that names no page, and a held out of range, are reported (GTO_ERR_BAD_INDEX); the row is copied as it is there.  The
  * outputs overlap neither one another nor the pool's arrays. */
 gto_status gto_pages_compact(gto_decode_ctx* ctx, const gto_page_pool* pool, const gto_kv_cache* cache,
                              int32_t* table_out, int32_t* ref_out, int32_t* n_used, void* stream);

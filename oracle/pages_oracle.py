@@ -1,7 +1,9 @@
 """Oracle of the page calls: one sequence and one page at a time, on the host.
 
 A pool is a dict of numpy int arrays page_table [S, max_pages], kv_len [S], held [S], ref_count [n_pages]; a cache is an
-array [n_layers, n_pages, page_size, ...].  The functions return new pools; `copies` lists (from, to, entries)."""
+array [n_layers, n_pages, page_size, ...].  The functions return new pools; `copies` lists (from, to, entries).  A sequence
+whose numbers do not allow the call stays as it is; what is given back need not be sound (a name that is no page is
+reported, and skipped)."""
 from __future__ import annotations
 
 import numpy as np

@@ -55,3 +55,70 @@ def test_compact_of_a_pool_without_sequences_refuses_what_it_would_write_over(gt
     inside = torch.zeros((3, 5), **I32)
     gto.gto_pages_compact(ctx, pool, k, v, inside[1:1], ref, used)  # nothing lies over anything
     assert gto.gto_decode_status(ctx) == 0
+
+
+# A page size of 4, 12 pages: sequence 0 holds pages 0 1 2 (9 entries), 1 holds 3 4 (5 entries), 2 and 3 nothing.
+TABLE, LEN, HELD = [[0, 1, 2, -1, -1], [3, 4, -1, -1, -1], [-1] * 5, [-1] * 5], [9, 5, 0, 0], [3, 2, 0, 0]
+COUNT = [1, 1, 1, 1, 1, 0, 0, 0, 0, 0, 0, 0]
+
+
+def broken(gto, cfg, **at):
+    pool = gto.alloc_page_pool(cfg, DEV)
+    for n, x in (("page_table", TABLE), ("kv_len", LEN), ("held", HELD), ("ref_count", COUNT)):
+        pool[n].copy_(torch.tensor(x))
+    for n, (where, value) in at.items():
+        pool[n][where] = value
+    return pool
+
+
+def numbers(pool):
+    return {n: x.tolist() for n, x in pool.items()}
+
+
+@pytest.mark.parametrize("call,give", [("fork", [0, -1, 2, 3]), ("fork", [0, 0, 2, 3]), ("resize", [-1, 0, -1, -1]), ("resize", [-1, 3, -1, -1])])
+def test_what_is_given_back_need_not_be_sound(gto, call, give):
+    """A slot that names no page is reported, the others are given back, and the call is carried out."""
+    ctx, cfg, k, v = make(gto)
+    do = lambda pool: gto.gto_pages_fork(ctx, pool, torch.tensor(give, **I32)) if call == "fork" else \
+        gto.gto_pages_resize(ctx, pool, torch.tensor(give, **I32), k, v)
+    whole = broken(gto, cfg)
+    do(whole)
+    assert gto.gto_decode_status(ctx) == 0 and whole["ref_count"][4].item() == 0
+    want = numbers(whole)
+    want["ref_count"][4] = 1                     # (its name is lost, its count stays)
+    for no_page in (-1, 12, 2 ** 31 - 1):
+        pool = broken(gto, cfg, page_table=((1, 1), no_page))
+        do(pool)
+        assert gto.gto_decode_status(ctx) == 8
+        assert numbers(pool) == want
+
+
+def test_what_the_page_calls_need_is_checked_before_anything_changes(gto):
+    ctx, cfg, k, v = make(gto)
+    for at in (dict(page_table=((1, 1), -1)), dict(page_table=((1, 1), 12)), dict(kv_len=(1, 9)), dict(held=(1, 6))):
+        pool = broken(gto, cfg, **at)
+        gto.gto_pages_fork(ctx, pool, torch.tensor([1, 1, 1, 3], **I32))     # 0 and 2 from 1, which is broken
+        assert gto.gto_decode_status(ctx) == 8 and numbers(pool) == numbers(broken(gto, cfg, **at))
+        for want in ([-1, 9, -1, -1], [-1, 20, -1, -1]):
+            gto.gto_pages_resize(ctx, pool, torch.tensor(want, **I32), k, v)
+            assert gto.gto_decode_status(ctx) == 8 and numbers(pool) == numbers(broken(gto, cfg, **at))
+    # its own length says nothing about a sequence that becomes another's copy
+    pool = broken(gto, cfg, kv_len=(1, 9))
+    gto.gto_pages_fork(ctx, pool, torch.tensor([0, 0, 2, 3], **I32))
+    assert gto.gto_decode_status(ctx) == 0
+    assert pool["held"].tolist() == [3, 3, 0, 0] and pool["kv_len"].tolist() == [9, 9, 0, 0]
+    assert pool["ref_count"].tolist() == [2, 2, 2] + [0] * 9
+    # slots that stay and are not written are not looked at
+    pool = broken(gto, cfg, page_table=((0, 0), 99))
+    gto.gto_pages_resize(ctx, pool, torch.tensor([16, -1, -1, -1], **I32), k, v)
+    assert gto.gto_decode_status(ctx) == 0 and pool["page_table"][0].tolist() == [99, 1, 2, 5, -1]
+
+
+@pytest.mark.parametrize("at", [dict(page_table=((0, 1), 12)), dict(held=(0, 6)), dict(held=(0, -1))])
+def test_compact_reports_a_row_that_is_broken_and_copies_it(gto, at):
+    ctx, cfg, k, v = make(gto)
+    pool = broken(gto, cfg, **at)
+    table, ref, used = torch.zeros((4, 5), **I32), torch.zeros(12, **I32), torch.zeros(1, **I32)
+    gto.gto_pages_compact(ctx, pool, k, v, table, ref, used)
+    assert gto.gto_decode_status(ctx) == 8 and used.item() == 5
+    assert torch.equal(table, pool["page_table"]) and torch.equal(ref, pool["ref_count"])
