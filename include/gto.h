@@ -544,7 +544,9 @@ gto_status gto_pages_resize(gto_decode_ctx* ctx, const gto_page_pool* pool, cons
 gto_status gto_pages_compact(gto_decode_ctx* ctx, const gto_page_pool* pool, const gto_kv_cache* cache,
                              int32_t* table_out, int32_t* ref_out, int32_t* n_used, void* stream);
 
-/* As gto_device_status and gto_launch_count, for a decoding context. */
+/* As gto_device_status and gto_launch_count, for a decoding context.  Of several faults since the last call one code tells, the
+ * first of GTO_ERR_TIMEOUT, GTO_ERR_BAD_INDEX, GTO_ERR_NO_PAGES and GTO_ERR_NONFINITE, and the others are cleared with it; but
+ * GTO_ERR_NO_PAGES neither hides another one nor is hidden: the next call then returns what is left. */
 gto_status gto_decode_status(gto_decode_ctx* ctx, void* stream, int32_t* host_code);
 int64_t gto_decode_launch_count(const gto_decode_ctx* ctx);
 

@@ -594,6 +594,12 @@ gto_status gto_decode_status(gto_decode_ctx* ctx, void* stream, int32_t* host_co
                : (word & gto::kStatusNoPages)   ? GTO_ERR_NO_PAGES
                : (word & gto::kStatusNonFinite) ? GTO_ERR_NONFINITE
                                                 : GTO_OK;
+  // too few pages neither hide other faults nor are hidden by them: one of the two is left for the next call
+  const int32_t others = word & ~gto::kStatusNoPages;
+  const int32_t rest = *host_code == GTO_ERR_NO_PAGES ? others : word & gto::kStatusNoPages;
+  if (rest != 0 && (cudaMemcpyAsync(ctx->status, &rest, sizeof(rest), cudaMemcpyHostToDevice, s) != cudaSuccess ||
+                    cudaStreamSynchronize(s) != cudaSuccess))
+    return GTO_ERR_CUDA;
   return GTO_OK;
 }
 

@@ -122,3 +122,31 @@ def test_compact_reports_a_row_that_is_broken_and_copies_it(gto, at):
     gto.gto_pages_compact(ctx, pool, k, v, table, ref, used)
     assert gto.gto_decode_status(ctx) == 8 and used.item() == 5
     assert torch.equal(table, pool["page_table"]) and torch.equal(ref, pool["ref_count"])
+
+
+def test_too_few_pages_are_told_beside_other_faults(gto):
+    """A caller that makes room and tries again has to be told, whatever else was wrong; and is told of that too."""
+    cfg = gto.make_decode_config(S=4, T=4, n_q_heads=1, n_kv_heads=1, head_dim=16, page_size=4, n_pages=12, max_pages=5, dtype="f32",
+                                 V_draft=64, V_target=64, logit_dtype="f32", flags=gto.GTO_DECODE_PAGES)
+    ctx = gto.gto_decode_create(cfg, 0)
+    k, v = (torch.zeros((12, 4, 1, 16), device=DEV) for _ in range(2))
+    want = lambda *n: torch.tensor(n, **I32)
+    draw = lambda heat: gto.gto_sample_tokens(ctx, torch.zeros((1, 64), device=DEV), dict(temperature=torch.tensor([heat], device=DEV)),
+                                              torch.zeros(1, device=DEV), torch.zeros(1, **I32))
+    status = lambda: [gto.gto_decode_status(ctx) for _ in range(3)]
+    short = want(20, 20, 20, 20)                                       # 20 pages of 12
+    pool = broken(gto, cfg)
+    gto.gto_pages_resize(ctx, pool, short, k, v)
+    assert status() == [9, 0, 0]
+    pool = broken(gto, cfg, kv_len=(0, 13))
+    gto.gto_pages_resize(ctx, pool, short, k, v)
+    assert status() == [8, 9, 0]
+    gto.gto_pages_resize(ctx, pool, short, k, v)
+    draw(-1.0)
+    assert status() == [8, 9, 0]                                       # (as ever: a bad index hides rows without a distribution)
+    pool = broken(gto, cfg)
+    gto.gto_pages_resize(ctx, pool, short, k, v)
+    draw(-1.0)
+    assert status() == [9, 5, 0]
+    draw(1.0)
+    assert status() == [0, 0, 0]
