@@ -485,7 +485,8 @@ typedef struct {
  * sum_{w <= v} p(w) > u[i], p being the distribution over what stays of row i of the logits, or of row rows[i]
  * (several sequences may draw from one row).  logits: [n_rows, V_target], row r at r * row_stride (elements, a multiple
  * of 16 bytes).  u: [N] fp32, given by the caller, in [0, 1) (clamped to it).  logp ([N] or NULL): log p(token); 0 at
- * temperature 0.  n_kept ([N] or NULL): how many tokens stay.  The decisions are those of fp64 sums.
+ * temperature 0; from fp64 sums and rounded once, but for a row without limits, whose mass may be an fp32 sum: off by 4.1e-6 at
+ * most.  n_kept ([N] or NULL): how many tokens stay.  The decisions are those of fp64 sums.
  * A sequence whose row holds NaN or +inf, or nothing but -inf, whose temperature is negative or not finite, or whose
  * top_p or min_p is NaN, is reported (GTO_ERR_NONFINITE), one whose rows[i] names no row too (GTO_ERR_BAD_INDEX); it
  * gets token -1, logp 0 and n_kept 0.  The outputs overlap neither one another nor what the call reads. */
