@@ -121,7 +121,7 @@ class DecodeStep:
         self.drawn = {"token": torch.zeros(cfg.S, dtype=torch.int32, device=self.device),
                       "logp": torch.zeros(cfg.S, dtype=torch.float32, device=self.device),
                       "n_kept": torch.zeros(cfg.S, dtype=torch.int32, device=self.device)}
-        self.pool = None
+        self.pool, self.moved = None, (None, None, None)
         if cfg.flags & gto.GTO_DECODE_PAGES:
             self.pool = dict(gto.alloc_page_pool(cfg, self.device), page_table=self.page_table, kv_len=self.kv_len)
             self.moved = (torch.empty_like(self.page_table), torch.empty_like(self.pool["ref_count"]),

@@ -150,3 +150,14 @@ def test_too_few_pages_are_told_beside_other_faults(gto):
     assert status() == [9, 5, 0]
     draw(1.0)
     assert status() == [0, 0, 0]
+
+
+def test_a_step_that_does_not_look_after_pages_refuses_the_page_calls(gto):
+    from paper_2509_22134_b200.runner import DecodeStep
+    cfg = gto.make_decode_config(S=2, T=2, n_q_heads=1, n_kv_heads=1, head_dim=16, page_size=4, n_pages=12, max_pages=5, dtype="f32",
+                                 V_draft=64, V_target=64, logit_dtype="f32")
+    step = DecodeStep(cfg, 1, [])
+    for call in (lambda: step.reserve(torch.zeros(2, **I32)), lambda: step.fork(torch.zeros(2, **I32)), step.compact):
+        with pytest.raises(ValueError):
+            call()
+    step.close()
