@@ -19,10 +19,10 @@
 //
 // Many rows have a CTA each, which leaves to a second kernel's clusters what the list or the fp32 sums cannot tell.
 //
-// What bounds it, as measured on a B200: a row of 128 256 bf16 of which a list's worth stays takes 12 us with its launch (eight
+// What bounds it, as measured on a B200: a row of 128 256 bf16 of which a list's worth stays takes 13 to 20 us with its launch (eight
 // CTAs: 3 us of reading, then a chain of some ten barriers and exchanges of 0.5 us each); one of which thousands stay 35 us,
 // most of it two more passes, one of shared-memory atomics and one of fp64 (64 lanes a cycle and SM, 20 instructions a
-// token).  512 such rows with mixed limits take 102 to 108 us (131 MB at 1.2 TB/s): the first kernel about 50 us, of which 20 us
+// token).  512 such rows with mixed limits take 101 to 109 us (131 MB at 1.2 TB/s): the first kernel about 50 us, of which 20 us
 // is the reading at 6.6 TB/s and 8 us the exponentials, the second about 55 us for the few per cent of rows that it is left.
 #pragma once
 

@@ -7,8 +7,8 @@
 // from the tables as they stood) and then its execution by another kernel, so that nothing is read after another
 // sequence has changed it.
 //
-// What bounds it, as measured on a B200: moving pages, the copy (a pool of 48 sequences of which 1.47 GB move: 470 us, 98 % of a
-// plain copy's rate); sharing and reserving, latency (6 us for two kernels that depend on one another at 4 sequences,
+// What bounds it, as measured on a B200: moving pages, the copy (a pool of 48 sequences of which 1.47 GB move: 470 to 498 us, 91 to
+// 97 % of a plain copy's rate); sharing and reserving, latency (6 us for two kernels that depend on one another at 4 sequences,
 // 16 us where one CTA numbers 256 sequences and searches a table of free pages: three rounds of loads
 // and block-wide sums, which a single CTA does without a barrier across the device).
 #include "decode_common.cuh"
